@@ -349,6 +349,108 @@ int cutoff_adam_step(int device, int64_t n, float* params, const float* grads, f
                      float beta1, float beta2, float eps, float clip_norm, float grad_scale, float* norm_out, void* workspace,
                      size_t workspace_bytes, void* stream);
 
+/* ---- layers of wider networks -----------------------------------------------------------------------
+ * The paper's networks have one hidden layer (Section 3.1.3).  These calls are what a residual block around wider or deeper
+ * ones is made of, on device buffers of the caller: dropout from the library's counter-based noise, the norms before and after a block
+ * with its gate and residual scale, and products in 8-bit integers.  All of them only enqueue work on `stream`, allocate nothing, give the
+ * same bits on every run and may be captured into a graph.  The paper has no counterpart.
+ *
+ * Matrices are row-major with a leading dimension (the distance between rows, in values, >= the row's length); what lies between a row's
+ * end and the next row is neither read as a value nor written.  An output may be the same matrix as an input of the same call (same address, leading
+ * dimension and type); other overlaps are undefined.  Values are `type`; parameters and their gradients are fp32.  Arithmetic and sums are fp32; an output
+ * is rounded once.  Rows that start on 16 bytes and have whole packs of 16 bytes are the fastest; nothing else depends on alignment except where
+ * said.  Zero rows are allowed; addresses are then not used, but NULL still means absent. */
+enum { CUTOFF_TYPE_FP32 = 0, CUTOFF_TYPE_FP16 = 1, CUTOFF_TYPE_BF16 = 2 };
+enum { CUTOFF_NORM_NONE = 0, CUTOFF_NORM_RMS = 1, CUTOFF_NORM_LAYER = 2 };
+enum { CUTOFF_GATE_LINEAR = 0, CUTOFF_GATE_SIGMOID = 1, CUTOFF_GATE_SILU = 2 };
+
+/* cutoff_dropout: y = residual + (kept ? x * 65536 / (65536 - T) : 0) with T = round(65536 p): the probability is a multiple of 2^-16, and the
+ * factor is the inverse of what is kept.  Element j of row i is kept if its 16 bits are >= T: with the Philox words of counter
+ * (j / 8, first_row + i, noise_stream, step) and key `seed` (the addressing of all noise here, see cutoff_debug_normals, with eight elements per
+ * counter), the low half of word (j % 8) / 2 for even j, the high half for odd j.  So the mask depends on neither the type nor the layout,
+ * is never stored, and is drawn again by the backward pass: the gradient with respect to x is the same call on the gradient of y without a
+ * residual.  Guide, transition and emission use the streams below 0x400.
+ *   x, y      device, rows x cols;  residual  device, rows x cols, or NULL for zeros
+ *   p         0 .. 1; with T = 65536 everything is dropped.  A dropped value is not looked at: NaN or infinity there do no harm.
+ *   first_row + rows <= 2^32.  Errors: BAD_ARG, CUDA. */
+int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, const void* residual,
+                   int64_t residual_ld, void* y, int64_t y_ld, double p, uint64_t seed, uint32_t step, uint32_t noise_stream, int64_t first_row,
+                   void* stream);
+
+/* The norms around a residual block.  With x the residual stream before the block and h the block's output, row by row
+ *     r = x + scale * act(gate) * post(h)          n = pre(r)
+ * where post and pre are CUTOFF_NORM_*: RMS v / sqrt(mean(v^2) + eps), LAYER (v - mean(v)) / sqrt(var(v) + eps) (population variance), times the weight
+ * plus the bias (NULL: ones, zeros), or NONE, which still applies weight and bias.  gate is a row for every gate_rows rows of x (1: one for each
+ * row; the last group may be shorter); act is CUTOFF_GATE_*: g, 1 / (1 + exp(-g)), g / (1 + exp(-g)).  NULL: gate 1, scale 1.  With h NULL
+ * there is no block: r = x (scale, gate, post_weight and post_bias must be NULL).  cols <= 8192 (TOO_LARGE otherwise), eps > 0.
+ *
+ * cutoff_residual_norm: residual (rows x cols, receives r; NULL = not wanted; must be NULL without h) and norm (receives n; NULL = not wanted).
+ * With norm_scale (rows floats) n is not stored as `type` but as 8-bit integers as cutoff_quantize_rows makes them of the unrounded n, norm being
+ * int8_t rows: what cutoff_quantized_product takes.
+ *
+ * cutoff_residual_norm_grad: given the gradients of a loss with respect to r and n (either may be NULL = zero), those with respect to the
+ * inputs.  Everything in grads is overwritten and may be NULL if it is not wanted; a gradient of something that the layer does not have must be NULL.
+ * The gate's gradient has the gate's shape (sums over the rows that share it), its type and all others' but the parameters' is `type`.  The forward pass
+ * is not needed before it: r and the statistics are formed again from x and h.  workspace: device, 16-byte aligned, at least
+ * cutoff_residual_norm_grad_workspace_bytes(rows, cols) bytes, contents undefined afterwards; calls that may overlap need one each.
+ * Errors: BAD_ARG, TOO_LARGE, CUDA (the workspace's size: BAD_ARG as a negative number). */
+typedef struct {
+    int64_t rows;
+    int32_t cols;
+    int32_t type;                       /* CUTOFF_TYPE_* of x, h, gate and what is computed from them */
+    const void* x;
+    int64_t x_ld;
+    const void* h;
+    int64_t h_ld;
+    const void* gate;                   /* ceil(rows / gate_rows) x cols */
+    int64_t gate_ld;
+    int64_t gate_rows;
+    int32_t gate_kind;                  /* CUTOFF_GATE_* */
+    int32_t post;                       /* CUTOFF_NORM_* */
+    int32_t pre;
+    float eps;
+    const float* scale;                 /* cols floats each, or NULL */
+    const float* post_weight;
+    const float* post_bias;
+    const float* pre_weight;
+    const float* pre_bias;
+} cutoff_norm_layer;
+
+typedef struct {
+    void* x;
+    int64_t x_ld;
+    void* h;
+    int64_t h_ld;
+    void* gate;
+    int64_t gate_ld;
+    float* scale;
+    float* post_weight;
+    float* post_bias;
+    float* pre_weight;
+    float* pre_bias;
+} cutoff_norm_grads;
+
+int cutoff_residual_norm(int device, const cutoff_norm_layer* layer, void* residual, int64_t residual_ld, void* norm, int64_t norm_ld,
+                         float* norm_scale, void* stream);
+int64_t cutoff_residual_norm_grad_workspace_bytes(int64_t rows, int32_t cols);
+int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const void* d_residual, int64_t d_residual_ld, const void* d_norm,
+                              int64_t d_norm_ld, const cutoff_norm_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Products in 8-bit integers with a scale for each row of either operand (token and output channel).
+ *
+ * cutoff_quantize_rows: scale[i] = max_j |x[i][j]| / 127, q[i][j] = rint(x[i][j] * (127 / max)) in single precision (ties to even), -127 .. 127.  A row
+ * of magnitudes below 2^-100 gives zeros; a row with a NaN or an infinity gives a scale that is NaN or infinite, and so NaN in its products.
+ *
+ * cutoff_quantized_product: y[i][j] = (sum_k a[i][k] b[j][k]) * a_scale[i] * b_scale[j] + bias[j], y m x n of `type`; the sum is exact.  a: m x k,
+ * b: n x k int8; both start on 16 bytes and their leading dimensions are multiples of 16 (BAD_ARG otherwise); whatever lies behind a row's k values
+ * is not used, but up to the next multiple of 16 it has to be readable.  bias: n floats or NULL.
+ * k <= CUTOFF_PRODUCT_MAX_K (TOO_LARGE otherwise: the sum could leave 32 bits).  Errors of both: BAD_ARG, TOO_LARGE, CUDA. */
+#define CUTOFF_PRODUCT_MAX_K 131071
+int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, int8_t* q, int64_t q_ld, float* scale,
+                         void* stream);
+int cutoff_quantized_product(int device, int64_t m, int32_t n, int32_t k, const int8_t* a, int64_t a_ld, const float* a_scale, const int8_t* b,
+                             int64_t b_ld, const float* b_scale, const float* bias, int32_t type, void* y, int64_t y_ld, void* stream);
+
 /* ---- allocation-free entry point ---------------------------------------------------------------
  * The paper has no counterpart for this call.  It serves programs that may not allocate device
  * memory at the time they need order statistics: a server that handed all of the GPU's memory to

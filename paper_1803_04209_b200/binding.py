@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+from typing import NamedTuple
 
 import numpy as np
 
@@ -20,6 +21,11 @@ OK, WARMUP, DEGENERATE = 0, 1, 2
 ERR_BAD_ARG, ERR_BAD_BLOB, ERR_BAD_VALUE, ERR_CUDA = -1, -2, -3, -4
 ERR_UNSUPPORTED, ERR_NOMEM, ERR_STATE, ERR_TIMEOUT, ERR_TOO_LARGE = -5, -6, -7, -8, -9
 STATIC_MAX_N = 1024
+PRODUCT_MAX_K = 131071
+TYPE_FP32, TYPE_FP16, TYPE_BF16 = 0, 1, 2
+NORMS = {None: 0, "rms": 1, "layer": 2}
+GATES = {"linear": 0, "sigmoid": 1, "silu": 2}
+STREAM_DROPOUT = 0x400          # first noise stream that no network of the library draws from
 PRECISION_FP32, PRECISION_TF32, PRECISION_BF16W = 0, 1, 2
 FLAG_GRAPH = 1
 FLAG_LITERAL = 2
@@ -36,6 +42,8 @@ EXPORTS = (
     "cutoff_decide_from_device_sums", "cutoff_measure_pipe_rates", "cutoff_measure_operand_stream", "cutoff_eval_trace", "cutoff_order_baseline",
     "cutoff_fit_param_count", "cutoff_fit_workspace_bytes", "cutoff_elbo_grad", "cutoff_adam_step",
     "cutoff_sorted_row_sums_static",
+    "cutoff_dropout", "cutoff_residual_norm", "cutoff_residual_norm_grad", "cutoff_residual_norm_grad_workspace_bytes",
+    "cutoff_quantize_rows", "cutoff_quantized_product",
 )
 
 
@@ -44,6 +52,22 @@ class CutoffConfig(C.Structure):
         ("n_workers", C.c_int32), ("latent_dim", C.c_int32), ("hidden", C.c_int32), ("lag", C.c_int32),
         ("n_samples", C.c_int32), ("precision", C.c_int32), ("device", C.c_int32), ("flags", C.c_int32),
         ("sample_offset", C.c_int64), ("total_samples", C.c_int64), ("stream", C.c_void_p), ("seed", C.c_uint64),
+    ]
+
+
+class NormLayer(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int64), ("cols", C.c_int32), ("type", C.c_int32), ("x", C.c_void_p), ("x_ld", C.c_int64), ("h", C.c_void_p),
+        ("h_ld", C.c_int64), ("gate", C.c_void_p), ("gate_ld", C.c_int64), ("gate_rows", C.c_int64), ("gate_kind", C.c_int32),
+        ("post", C.c_int32), ("pre", C.c_int32), ("eps", C.c_float), ("scale", C.c_void_p), ("post_weight", C.c_void_p),
+        ("post_bias", C.c_void_p), ("pre_weight", C.c_void_p), ("pre_bias", C.c_void_p),
+    ]
+
+
+class NormGrads(C.Structure):
+    _fields_ = [
+        ("x", C.c_void_p), ("x_ld", C.c_int64), ("h", C.c_void_p), ("h_ld", C.c_int64), ("gate", C.c_void_p), ("gate_ld", C.c_int64),
+        ("scale", C.c_void_p), ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("pre_weight", C.c_void_p), ("pre_bias", C.c_void_p),
     ]
 
 
@@ -113,6 +137,14 @@ def load_library(path: str | None = None) -> C.CDLL:
         "cutoff_adam_step": (C.c_int, [C.c_int, C.c_int64, vp, vp, vp, vp, C.c_int32, C.c_float, C.c_float, C.c_float,
                                        C.c_float, C.c_float, C.c_float, vp, vp, C.c_size_t, vp]),
         "cutoff_sorted_row_sums_static": (C.c_int, [C.c_int, vp, C.c_int64, C.c_int32, C.c_int32, vp, vp]),
+        "cutoff_dropout": (C.c_int, [C.c_int, C.c_int32, C.c_int64, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, C.c_double, C.c_uint64,
+                                     C.c_uint32, C.c_uint32, C.c_int64, vp]),
+        "cutoff_residual_norm": (C.c_int, [C.c_int, C.POINTER(NormLayer), vp, C.c_int64, vp, C.c_int64, vp, vp]),
+        "cutoff_residual_norm_grad": (C.c_int, [C.c_int, C.POINTER(NormLayer), vp, C.c_int64, vp, C.c_int64, C.POINTER(NormGrads), vp, C.c_size_t, vp]),
+        "cutoff_residual_norm_grad_workspace_bytes": (C.c_int64, [C.c_int64, C.c_int32]),
+        "cutoff_quantize_rows": (C.c_int, [C.c_int, C.c_int32, C.c_int64, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp, vp]),
+        "cutoff_quantized_product": (C.c_int, [C.c_int, C.c_int64, C.c_int32, C.c_int32, vp, C.c_int64, vp, vp, C.c_int64, vp, vp, C.c_int32, vp,
+                                               C.c_int64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)          # AttributeError if the library does not export it
@@ -506,6 +538,195 @@ class Fitter:
 
     def weights(self) -> dict:
         return unflatten_weights(self.params.cpu().numpy(), self.N, self.D, self.H)
+
+
+# ---- layers of wider networks ----------------------------------------------------------------------------------------
+# Matrices are two-dimensional CUDA tensors (fp32, fp16 or bf16) whose rows are contiguous; rows may be further apart than they are long.
+# Parameters are contiguous fp32 vectors.  Work goes to torch's current stream of the tensors' device.
+
+class Quantized(NamedTuple):
+    """Rows of 8-bit integers and the scale of each row: value = integer * scale."""
+    values: object                  # int8 [rows, cols], rows on 16-byte boundaries
+    scale: object                   # fp32 [rows]
+
+
+def _type_of(t) -> int:
+    import torch
+    code = {torch.float32: TYPE_FP32, torch.float16: TYPE_FP16, torch.bfloat16: TYPE_BF16}.get(t.dtype)
+    if code is None:
+        raise ValueError(f"expected a tensor of fp32, fp16 or bf16 values, not {t.dtype}")
+    return code
+
+
+def _matrix(t, what: str, like=None, rows: int | None = None, dtype=None):
+    """(address, leading dimension) of a matrix; `like`: the matrix whose device, columns, type and (unless `rows` is given) rows it has to have."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or not t.is_cuda or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: expected a CUDA matrix [rows, columns] with contiguous rows")
+    if like is not None and (t.device != like.device or t.shape[1] != like.shape[1] or t.shape[0] != (like.shape[0] if rows is None else rows) or
+                             t.dtype != (like.dtype if dtype is None else dtype)):
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device} does not fit {like.dtype} {tuple(like.shape)} on {like.device}")
+    n, cols = t.shape
+    if n <= 1:
+        # the distance to a row that there is not may be anything, and so may the address of no rows (torch says 0, which would read as "absent")
+        return t.data_ptr() or 16, max(t.stride(0), cols)
+    if t.stride(0) < cols:
+        raise ValueError(f"{what}: rows overlap")
+    return t.data_ptr(), t.stride(0)
+
+
+def _vector(t, what: str, like, n: int):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.device != like.device or tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous fp32 vector of {n} values on {like.device}")
+    return t.data_ptr() or 16
+
+
+def _stream_of(t):
+    import torch
+    return t.device.index, torch.cuda.current_stream(t.device).cuda_stream
+
+
+def dropout(x, p: float, seed: int, step: int = 0, noise_stream: int = STREAM_DROPOUT, first_row: int = 0, residual=None, out=None):
+    """residual + (kept ? x / (1 - p) : 0); the mask is a function of (seed, step, noise_stream, first_row + row, column) and never stored.
+
+    The gradient with respect to x is dropout(gradient of the result, p, seed, step, noise_stream, first_row); that with respect to the
+    residual is the gradient of the result.  p counts in steps of 2^-16.  out may be x or residual."""
+    import torch
+    lib = load_library()
+    xp, x_ld = _matrix(x, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    rp, r_ld = _matrix(residual, "residual", x)
+    op, o_ld = _matrix(out, "out", x)
+    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= noise_stream < 1 << 32):
+        raise ValueError("seed has 64 bits, step and noise_stream 32")
+    device, stream = _stream_of(x)
+    rc = lib.cutoff_dropout(device, _type_of(x), x.shape[0], x.shape[1], xp, x_ld, rp, r_ld, op, o_ld, p, seed, step, noise_stream, first_row, stream)
+    if rc < 0:
+        raise CutoffError(rc, "cutoff_dropout")
+    return out
+
+
+def _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps):
+    if post not in NORMS or pre not in NORMS or gate_kind not in GATES:
+        raise ValueError(f"norms: {list(NORMS)}, gates: {list(GATES)}")
+    if gate_rows < 1:
+        raise ValueError("gate_rows is at least 1")
+    xp, x_ld = _matrix(x, "x")
+    hp, h_ld = _matrix(h, "h", x)
+    rows, cols = x.shape
+    gp, g_ld = _matrix(gate, "gate", x, rows=-(-rows // gate_rows))
+    return NormLayer(rows, cols, _type_of(x), xp, x_ld, hp, h_ld, gp, g_ld, gate_rows, GATES[gate_kind], NORMS[post], NORMS[pre], eps,
+                     _vector(scale, "scale", x, cols), _vector(post_weight, "post_weight", x, cols), _vector(post_bias, "post_bias", x, cols),
+                     _vector(pre_weight, "pre_weight", x, cols), _vector(pre_bias, "pre_bias", x, cols))
+
+
+def residual_norm(x, h=None, gate=None, gate_rows: int = 1, gate_kind: str = "linear", scale=None, post: str | None = "rms", post_weight=None,
+                  post_bias=None, pre: str | None = "rms", pre_weight=None, pre_bias=None, eps: float = 1e-6, want_norm: bool = True,
+                  quantize: bool = False, residual_out=None, norm_out=None):
+    """(r, n): r = x + scale * act(gate) * post(h), n = pre(r).
+
+    x, h [rows, cols]; gate [ceil(rows / gate_rows), cols]; post, pre: "rms", "layer" or None, with weights and biases [cols].  Without h there is no
+    block before: r is x.  With want_norm=False n is None.  With quantize=True n is a Quantized of 8-bit rows, as quantized_product takes them.
+    residual_out and norm_out may be x or h."""
+    import torch
+    lib = load_library()
+    layer = _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps)
+    rows, cols = x.shape
+    r, rp, r_ld, n, np_, n_ld, sp = x, None, 0, None, None, 0, None
+    if h is not None:
+        r = torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual_out is None else residual_out
+        rp, r_ld = _matrix(r, "residual_out", x)
+    if want_norm and quantize:
+        n = _empty_quantized(rows, cols, x.device)
+        np_, n_ld, sp = n.values.data_ptr() or 16, (cols + 15) // 16 * 16, n.scale.data_ptr() or 16
+    elif want_norm:
+        n = torch.empty(x.shape, dtype=x.dtype, device=x.device) if norm_out is None else norm_out
+        np_, n_ld = _matrix(n, "norm_out", x)
+    device, stream = _stream_of(x)
+    rc = lib.cutoff_residual_norm(device, C.byref(layer), rp, r_ld, np_, n_ld, sp, stream)
+    if rc < 0:
+        raise CutoffError(rc, "cutoff_residual_norm")
+    return r, n
+
+
+def residual_norm_grad(x, h, d_residual, d_norm, gate=None, gate_rows: int = 1, gate_kind: str = "linear", scale=None, post: str | None = "rms",
+                       post_weight=None, post_bias=None, pre: str | None = "rms", pre_weight=None, pre_bias=None, eps: float = 1e-6) -> dict:
+    """The gradients of residual_norm's inputs ("x", and of "h", "gate", "scale", "post_weight", "post_bias", "pre_weight", "pre_bias" those that
+    there are), given those of a loss with respect to r and n (either may be None).  x and h are the forward pass's inputs; nothing of its
+    results is needed."""
+    import torch
+    lib = load_library()
+    layer = _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps)
+    rows, cols = x.shape
+    rp, r_ld = _matrix(d_residual, "d_residual", x)
+    np_, n_ld = _matrix(d_norm, "d_norm", x)
+    out = {"x": torch.empty(x.shape, dtype=x.dtype, device=x.device)}
+    for name, t in (("h", h), ("gate", gate), ("scale", scale), ("post_weight", post_weight), ("post_bias", post_bias), ("pre_weight", pre_weight),
+                    ("pre_bias", pre_bias)):
+        if t is not None:
+            out[name] = torch.empty(t.shape, dtype=t.dtype, device=x.device)
+
+    def at(name):
+        return out[name].data_ptr() or 16 if name in out else None
+    grads = NormGrads(at("x"), cols, at("h"), cols, at("gate"), cols, at("scale"), at("post_weight"), at("post_bias"), at("pre_weight"), at("pre_bias"))
+    need = lib.cutoff_residual_norm_grad_workspace_bytes(rows, cols)
+    ws = torch.empty(max(need, 256), dtype=torch.uint8, device=x.device)
+    device, stream = _stream_of(x)
+    rc = lib.cutoff_residual_norm_grad(device, C.byref(layer), rp, r_ld, np_, n_ld, C.byref(grads), ws.data_ptr(), ws.numel(), stream)
+    if rc < 0:
+        raise CutoffError(rc, "cutoff_residual_norm_grad")
+    return out
+
+
+def _empty_quantized(rows: int, cols: int, device) -> Quantized:
+    import torch
+    values = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)
+    return Quantized(values[:, :cols], torch.empty(rows, dtype=torch.float32, device=device))
+
+
+def quantize_rows(x) -> Quantized:
+    """8-bit integers of each row of x and their scale (largest magnitude / 127): the tokens of a product, or once its weights [outputs, inputs]."""
+    lib = load_library()
+    xp, x_ld = _matrix(x, "x")
+    rows, cols = x.shape
+    q = _empty_quantized(rows, cols, x.device)
+    if rows == 0:
+        return q
+    device, stream = _stream_of(x)
+    rc = lib.cutoff_quantize_rows(device, _type_of(x), rows, cols, xp, x_ld, q.values.data_ptr(), (cols + 15) // 16 * 16, q.scale.data_ptr(), stream)
+    if rc < 0:
+        raise CutoffError(rc, "cutoff_quantize_rows")
+    return q
+
+
+def quantized_product(a, b, bias=None, dtype=None, out=None):
+    """a b^T of two Quantized (or pairs of int8 rows and fp32 scales): a [m, k] tokens, b [n, k] weights; plus bias [n].
+
+    Returns [m, n] of `dtype` (bf16 if neither it nor `out` is given).  The integer sums are exact.  Rows of a and b start on 16-byte boundaries."""
+    import torch
+    lib = load_library()
+    (av, a_scale), (bv, b_scale) = a, b
+    ap, a_ld = _matrix(av, "a")
+    bp, b_ld = _matrix(bv, "b", av, rows=bv.shape[0])
+    if av.dtype != torch.int8:
+        raise ValueError("expected rows of int8 values")
+    m, n, k = av.shape[0], bv.shape[0], av.shape[1]
+    if out is None:
+        out = torch.empty((m, n), dtype=dtype or torch.bfloat16, device=av.device)
+    elif tuple(out.shape) != (m, n) or out.device != av.device or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out: expected [{m}, {n}] on {av.device}")
+    op, o_ld = _matrix(out, "out")
+    device, stream = _stream_of(av)
+    rc = lib.cutoff_quantized_product(device, m, n, k, ap, a_ld, _vector(a_scale, "a's scale", av, m), bp, b_ld, _vector(b_scale, "b's scale", av, n),
+                                      _vector(bias, "bias", av, n), _type_of(out), op, o_ld, stream)
+    if rc < 0:
+        raise CutoffError(rc, "cutoff_quantized_product")
+    return out
 
 
 def sorted_row_sums_static(x, sums, n: int | None = None, stream: int | None = None) -> int:

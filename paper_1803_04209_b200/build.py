@@ -9,10 +9,10 @@ import sys
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libcutoff.so")
-SOURCES = ["cutoff_api.cu"]
+SOURCES = ["cutoff_api.cu", "layers_api.cu", "norm_fp32.cu", "norm_fp16.cu", "norm_bf16.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-shared", "-Xcompiler", "-fPIC",
+    "-shared", "-Xcompiler", "-fPIC", "-t", "0",      # the sources side by side
 ]
 
 

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "launch.cuh"
 #include "kernels_model.cuh"
 #include "kernels_sort.cuh"
 #include "bucket_sort.cuh"
@@ -145,26 +146,6 @@ namespace {
         }                                                                                            \
     } while (0)
 
-// Makes the context's device current for the duration of an entry point and puts the caller's
-// current device back on exit.
-struct DeviceGuard {
-    int prev = -1;
-    bool changed = false;
-    cudaError_t err = cudaSuccess;
-    explicit DeviceGuard(int device) {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        if (prev != device) {
-            err = cudaSetDevice(device);
-            changed = err == cudaSuccess;
-        }
-    }
-    ~DeviceGuard() {
-        if (changed && prev >= 0) cudaSetDevice(prev);
-    }
-    DeviceGuard(const DeviceGuard&) = delete;
-    DeviceGuard& operator=(const DeviceGuard&) = delete;
-};
-
 std::vector<TensorSpec> tensor_specs(size_t N, size_t D, size_t H) {
     return {
         {"Wxf", H, N}, {"Whf", H, H}, {"bf", 1, H}, {"a0", 1, H},
@@ -263,23 +244,6 @@ void layer_bound(const float* w, const float* b, size_t rows, size_t cols, bool 
     }
     bound[0] = static_cast<float>(l1 * 1.001);
     bound[1] = static_cast<float>(mb * 1.001);
-}
-
-// Launch `kernel` so that it may begin while the kernel before it in the stream is still running (programmatic
-// dependent launch): the kernel itself waits, by dependency_wait(), before it touches that kernel's results.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args&&... args) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
 int next_pow2(int n) {

@@ -1,0 +1,250 @@
+// C entry points of the layer operators (see include/cutoff.h): arguments are checked, a kernel is chosen by sizes, types and alignment,
+// work is enqueued.
+#include "../../include/cutoff.h"
+
+#include <cmath>
+#include <type_traits>
+
+#include "launch.cuh"
+#include "dropout.cuh"
+#include "residual_norm.cuh"
+#include "int8_product.cuh"
+
+using namespace cutoff;
+using namespace cutoff::layers;
+
+namespace {
+
+constexpr int kMostCols = 8192;               // of a norm
+constexpr int kMostDevices = 64;
+
+int status() { return cudaGetLastError() == cudaSuccess ? CUTOFF_OK : CUTOFF_ERR_CUDA; }
+
+int sm_count(int device) {
+    static int sms[kMostDevices] = {};
+    if (device >= kMostDevices) return 148;
+    if (!sms[device]) {
+        int v = 0;
+        if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || v < 1) return 148;
+        sms[device] = v;
+    }
+    return sms[device];
+}
+
+bool known_type(int32_t type) { return type == CUTOFF_TYPE_FP32 || type == CUTOFF_TYPE_FP16 || type == CUTOFF_TYPE_BF16; }
+int type_size(int32_t type) { return type == CUTOFF_TYPE_FP32 ? 4 : 2; }
+
+// f(a value of the element type)
+template <typename F>
+void with_type(int32_t type, F f) {
+    if (type == CUTOFF_TYPE_FP32) f(float{});
+    else if (type == CUTOFF_TYPE_FP16) f(__half{});
+    else f(__nv_bfloat16{});
+}
+
+// Whether every row of a matrix starts on a multiple of `bytes` (a null matrix does).
+bool rows_aligned(const void* p, int64_t ld, int size, int bytes) {
+    return p == nullptr || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % bytes == 0);
+}
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool bad_matrix(const void* p, int64_t ld, int64_t cols) { return p != nullptr && ld < cols; }
+
+// ---- dropout ---------------------------------------------------------------------------------------------------------
+template <typename T, int V, int LX>
+void launch_dropout(const DropoutArgs& a, int sms, cudaStream_t s) {
+    constexpr int kUnroll = 2, kWarps = kDropoutThreads / 32;
+    const int64_t row_warps = ceil_div64(a.rows, kUnroll * (32 / LX));     // warps that find work in a tile of columns
+    const int64_t resident = static_cast<int64_t>(sms) * 4 * kWarps;
+    int64_t each = resident / a.tiles;
+    each = each < 1 ? 1 : each < row_warps ? each : row_warps;
+    k_dropout<T, V, LX, kUnroll><<<static_cast<unsigned>(ceil_div64(each * a.tiles, kWarps)), kDropoutThreads, 0, s>>>(a);
+}
+template <typename T, int V>
+void launch_dropout(DropoutArgs& a, int sms, cudaStream_t s) {
+    const int groups = ceil_div(a.cols, 8);
+    const auto run = [&](auto lanes) {
+        constexpr int LX = decltype(lanes)::value;
+        a.tiles = ceil_div(groups, LX);
+        launch_dropout<T, V, LX>(a, sms, s);
+    };
+    if (groups <= 2) run(std::integral_constant<int, 2>{});
+    else if (groups <= 8) run(std::integral_constant<int, 8>{});
+    else run(std::integral_constant<int, 32>{});
+}
+
+// ---- norms -----------------------------------------------------------------------------------------------------------
+bool bad_layer(const cutoff_norm_layer* l) {
+    return !l || l->rows < 0 || l->rows > INT32_MAX || l->cols < 1 || !known_type(l->type) || !l->x || l->x_ld < l->cols || bad_matrix(l->h, l->h_ld, l->cols) ||
+           bad_matrix(l->gate, l->gate_ld, l->cols) || (l->gate && (l->gate_rows < 1 || !l->h)) || l->gate_kind < CUTOFF_GATE_LINEAR ||
+           l->gate_kind > CUTOFF_GATE_SILU || l->post < CUTOFF_NORM_NONE || l->post > CUTOFF_NORM_LAYER || l->pre < CUTOFF_NORM_NONE ||
+           l->pre > CUTOFF_NORM_LAYER || !(l->eps > 0.f) || !std::isfinite(l->eps) || (!l->h && (l->scale || l->post_weight || l->post_bias));
+}
+
+NormArgs norm_args(const cutoff_norm_layer* l) {
+    NormArgs a{};
+    a.x = l->x; a.h = l->h; a.gate = l->gate;
+    a.scale = l->scale; a.post_w = l->post_weight; a.post_b = l->post_bias; a.pre_w = l->pre_weight; a.pre_b = l->pre_bias;
+    a.rows = l->rows; a.x_ld = l->x_ld; a.h_ld = l->h_ld; a.gate_ld = l->gate_ld; a.gate_rows = l->gate_rows;
+    a.cols = l->cols; a.gate_kind = l->gate_kind; a.post = l->post; a.pre = l->pre;
+    a.eps = l->eps; a.inv_cols = 1.f / static_cast<float>(l->cols);
+    return a;
+}
+bool whole_packs(const cutoff_norm_layer* l) {
+    const int size = type_size(l->type);
+    return l->cols * size % 16 == 0 && rows_aligned(l->x, l->x_ld, size, 16) && rows_aligned(l->h, l->h_ld, size, 16) &&
+           rows_aligned(l->gate, l->gate_ld, size, 16) && aligned16(l->scale) && aligned16(l->post_weight) && aligned16(l->post_bias) &&
+           aligned16(l->pre_weight) && aligned16(l->pre_bias);
+}
+
+// Teams of the backward pass: as many as are resident, but so that none adds more than kMostTeamRows rows in a row.
+constexpr int64_t kMostTeamRows = 1024;
+GradPlan grad_plan(int64_t rows, int cols, int sms) {
+    const int per_cta = cols <= 32 ? kNormWarpThreads / 4 : cols <= 128 ? kNormWarpThreads / 16 : cols <= 512 ? kNormWarpThreads / 32 : 1;
+    int64_t ctas = static_cast<int64_t>(sms) * (cols <= 512 ? 2 : 2);
+    const int64_t few = ceil_div64(rows, per_cta), many = ceil_div64(rows, kMostTeamRows * per_cta);
+    ctas = ctas < many ? many : ctas;
+    ctas = ctas < few ? ctas : few;
+    return GradPlan{ctas, ctas * per_cta};
+}
+
+// ---- products --------------------------------------------------------------------------------------------------------
+template <typename T>
+void launch_product(const ProductArgs& p, cudaStream_t s) {
+    const auto run = [&](auto rows) {
+        constexpr int MT = decltype(rows)::value;
+        launch_dependent(k_product_dot<T, MT>, dim3(ceil_div(p.n, kDotWarps), static_cast<unsigned>(ceil_div64(p.m, MT))), dim3(kDotWarps * 32), 0, s, p);
+    };
+    if (p.m == 1) run(std::integral_constant<int, 1>{});
+    else run(std::integral_constant<int, 8>{});
+}
+
+}  // namespace
+
+extern "C" {
+
+int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, const void* residual, int64_t residual_ld,
+                   void* y, int64_t y_ld, double p, uint64_t seed, uint32_t step, uint32_t noise_stream, int64_t first_row, void* stream) {
+    if (device < 0 || !known_type(type) || rows < 0 || cols < 1 || !x || !y || x_ld < cols || y_ld < cols || bad_matrix(residual, residual_ld, cols) ||
+        !(p >= 0.0 && p <= 1.0) || first_row < 0 || rows > (int64_t{1} << 32) || first_row > (int64_t{1} << 32) - rows)
+        return CUTOFF_ERR_BAD_ARG;
+    if (rows == 0) return CUTOFF_OK;
+    DeviceGuard guard(device);
+    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    const uint32_t dropped = static_cast<uint32_t>(std::nearbyint(p * 65536.0));
+    DropoutArgs a{};
+    a.x = x; a.residual = residual; a.y = y;
+    a.rows = rows; a.x_ld = x_ld; a.residual_ld = residual_ld; a.y_ld = y_ld; a.cols = cols;
+    a.first_row = static_cast<uint32_t>(first_row); a.stream = noise_stream; a.step = step;
+    a.key = NoiseKey{static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32)};
+    a.border = dropped < 65536 ? dropped << 16 : 0xffffffffu;
+    a.word_mask = dropped < 65536 ? 0xffffffffu : 0u;
+    a.scale = dropped < 65536 ? static_cast<float>(65536.0 / (65536 - dropped)) : 0.f;
+    const int size = type_size(type);
+    const bool packs = cols * static_cast<int64_t>(size) % 16 == 0 && rows_aligned(x, x_ld, size, 16) && rows_aligned(residual, residual_ld, size, 16) &&
+                       rows_aligned(y, y_ld, size, 16);
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        if (packs) launch_dropout<T, kPack<T>>(a, sm_count(device), static_cast<cudaStream_t>(stream));
+        else launch_dropout<T, 1>(a, sm_count(device), static_cast<cudaStream_t>(stream));
+    });
+    return status();
+}
+
+int cutoff_residual_norm(int device, const cutoff_norm_layer* layer, void* residual, int64_t residual_ld, void* norm, int64_t norm_ld, float* norm_scale,
+                         void* stream) {
+    if (device < 0 || bad_layer(layer) || bad_matrix(residual, residual_ld, layer->cols) || bad_matrix(norm, norm_ld, layer->cols) ||
+        (!residual && !norm) || (!layer->h && residual) || (norm_scale && !norm))
+        return CUTOFF_ERR_BAD_ARG;
+    if (layer->cols > kMostCols) return CUTOFF_ERR_TOO_LARGE;
+    if (layer->rows == 0) return CUTOFF_OK;
+    DeviceGuard guard(device);
+    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    NormArgs a = norm_args(layer);
+    a.r = residual; a.n = norm; a.n_scale = norm_scale; a.r_ld = residual_ld; a.n_ld = norm_ld;
+    const int size = type_size(layer->type);
+    const bool packs = whole_packs(layer) && rows_aligned(residual, residual_ld, size, 16) &&
+                       (norm_scale ? rows_aligned(norm, norm_ld, 1, 16 / size) : rows_aligned(norm, norm_ld, size, 16));
+    with_type(layer->type, [&](auto t) {
+        using T = decltype(t);
+        run_norm<T>(a, packs, static_cast<cudaStream_t>(stream));
+    });
+    return status();
+}
+
+int64_t cutoff_residual_norm_grad_workspace_bytes(int64_t rows, int32_t cols) {
+    if (rows < 0 || rows > INT32_MAX || cols < 1 || cols > kMostCols) return CUTOFF_ERR_BAD_ARG;
+    const GradPlan plan = grad_plan(rows, cols, 256);        // for a GPU of up to 256 SMs
+    return (4 * plan.ctas + 2 * plan.teams) * cols * static_cast<int64_t>(sizeof(float)) + 256;
+}
+
+int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const void* d_residual, int64_t d_residual_ld, const void* d_norm,
+                              int64_t d_norm_ld, const cutoff_norm_grads* grads, void* workspace, size_t workspace_bytes, void* stream) {
+    if (device < 0 || bad_layer(layer) || !grads || bad_matrix(d_residual, d_residual_ld, layer->cols) || bad_matrix(d_norm, d_norm_ld, layer->cols) ||
+        (!d_residual && !d_norm) || bad_matrix(grads->x, grads->x_ld, layer->cols) || bad_matrix(grads->h, grads->h_ld, layer->cols) ||
+        bad_matrix(grads->gate, grads->gate_ld, layer->cols) || (!layer->h && (grads->h || grads->gate)) || (grads->gate && !layer->gate) || !workspace ||
+        (grads->scale && !layer->scale) || (grads->post_weight && !layer->post_weight) || (grads->post_bias && !layer->post_bias) ||
+        (grads->pre_weight && !layer->pre_weight) || (grads->pre_bias && !layer->pre_bias))
+        return CUTOFF_ERR_BAD_ARG;
+    if (layer->cols > kMostCols) return CUTOFF_ERR_TOO_LARGE;
+    if (static_cast<int64_t>(workspace_bytes) < cutoff_residual_norm_grad_workspace_bytes(layer->rows, layer->cols) || !aligned16(workspace))
+        return CUTOFF_ERR_BAD_ARG;
+    DeviceGuard guard(device);
+    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int sms = sm_count(device);
+    const GradPlan plan = grad_plan(layer->rows, layer->cols, sms < 256 ? sms : 256);
+    const bool bias = layer->post_bias || layer->pre_bias, groups = layer->gate && layer->gate_rows > 1;
+    NormFinishArgs q{};
+    NormGradArgs& g = q.g;
+    g.f = norm_args(layer);
+    g.d_r = d_residual; g.d_n = d_norm; g.d_r_ld = d_residual_ld; g.d_n_ld = d_norm_ld;
+    g.d_x = grads->x; g.d_h = grads->h; g.d_gate = grads->gate; g.d_x_ld = grads->x_ld; g.d_h_ld = grads->h_ld; g.d_gate_ld = grads->gate_ld;
+    g.sums = static_cast<float*>(workspace);
+    g.gate_sums = g.sums + 4 * plan.ctas * layer->cols;
+    g.teams = plan.teams;
+    q.ctas = static_cast<int>(plan.ctas); q.each = bias ? 4 : 2;
+    q.d_scale = grads->scale; q.d_post_w = grads->post_weight; q.d_post_b = grads->post_bias; q.d_pre_w = grads->pre_weight; q.d_pre_b = grads->pre_bias;
+    const int size = type_size(layer->type);
+    const bool packs = whole_packs(layer) && rows_aligned(d_residual, d_residual_ld, size, 16) && rows_aligned(d_norm, d_norm_ld, size, 16) &&
+                       rows_aligned(grads->x, grads->x_ld, size, 16) && rows_aligned(grads->h, grads->h_ld, size, 16) &&
+                       rows_aligned(grads->gate, grads->gate_ld, size, 16);
+    const bool sums = grads->scale || grads->post_weight || grads->post_bias || grads->pre_weight || grads->pre_bias;
+    q.column_blocks = sums ? ceil_div(layer->cols, kFinishColumns) : 0;
+    const int gate_blocks = groups && grads->gate && layer->rows > 0 ? static_cast<int>(plan.teams < 2 * sms ? plan.teams : 2 * sms) : 0;
+    with_type(layer->type, [&](auto t) { run_norm_grad<decltype(t)>(q, plan, packs, bias, groups, q.column_blocks + gate_blocks, s); });
+    return status();
+}
+
+int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, int8_t* q, int64_t q_ld, float* scale,
+                         void* stream) {
+    if (device < 0 || !known_type(type) || rows < 0 || rows > INT32_MAX || cols < 1 || !x || !q || !scale || x_ld < cols || q_ld < cols)
+        return CUTOFF_ERR_BAD_ARG;
+    if (rows == 0) return CUTOFF_OK;
+    DeviceGuard guard(device);
+    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    const QuantizeArgs a{x, q, scale, rows, x_ld, q_ld, cols};
+    const int size = type_size(type);
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        const bool packs = cols % kPack<T> == 0 && rows_aligned(x, x_ld, size, 16) && rows_aligned(q, q_ld, 1, kPack<T>);
+        launch_dependent(packs ? k_quantize_rows<T, kPack<T>> : k_quantize_rows<T, 1>, dim3(static_cast<unsigned>(rows)), dim3(kQuantizeThreads), 0,
+                         static_cast<cudaStream_t>(stream), a);
+    });
+    return status();
+}
+
+int cutoff_quantized_product(int device, int64_t m, int32_t n, int32_t k, const int8_t* a, int64_t a_ld, const float* a_scale, const int8_t* b,
+                             int64_t b_ld, const float* b_scale, const float* bias, int32_t type, void* y, int64_t y_ld, void* stream) {
+    if (device < 0 || m < 0 || m > INT32_MAX || n < 1 || k < 1 || !a || !a_scale || !b || !b_scale || !known_type(type) || !y || a_ld < k || b_ld < k || y_ld < n ||
+        !rows_aligned(a, a_ld, 1, 16) || !rows_aligned(b, b_ld, 1, 16))
+        return CUTOFF_ERR_BAD_ARG;
+    if (k > CUTOFF_PRODUCT_MAX_K) return CUTOFF_ERR_TOO_LARGE;
+    if (m == 0) return CUTOFF_OK;
+    DeviceGuard guard(device);
+    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    const ProductArgs p{a, b, a_scale, b_scale, bias, y, m, a_ld, b_ld, y_ld, n, k};
+    with_type(type, [&](auto t) { launch_product<decltype(t)>(p, static_cast<cudaStream_t>(stream)); });
+    return status();
+}
+
+}  // extern "C"

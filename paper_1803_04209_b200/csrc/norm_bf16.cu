@@ -1,0 +1,9 @@
+// The norm kernels of bf16 values.
+#include "norm_launch.cuh"
+
+namespace cutoff {
+namespace layers {
+template void run_norm<__nv_bfloat16>(const NormArgs&, bool, cudaStream_t);
+template void run_norm_grad<__nv_bfloat16>(const NormFinishArgs&, const GradPlan&, bool, bool, bool, int, cudaStream_t);
+}  // namespace layers
+}  // namespace cutoff
