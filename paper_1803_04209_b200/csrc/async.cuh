@@ -1,6 +1,6 @@
 // mbarrier and bulk-copy primitives shared by the kernels that use the asynchronous copy engine.
 // Every wait is bounded: it gives up after kWaitLimitNs, records kErrTimeout in the device state
-// and tells the rest of the CTA through an abort flag in shared memory.
+// (unless there is none: a null pointer) and tells the rest of the CTA through an abort flag in shared memory.
 #pragma once
 #include <cstdint>
 
@@ -54,7 +54,7 @@ __device__ __forceinline__ void mbar_wait_lane(uint32_t bar, uint32_t parity, vo
             if (*abort_flag) return;
             if (global_ns() - t0 > kWaitLimitNs) {
                 *abort_flag = 1;
-                atomicOr(&st->error_flags, kErrTimeout);
+                if (st) atomicOr(&st->error_flags, kErrTimeout);
                 return;
             }
         }
@@ -73,7 +73,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
             if (__any_sync(0xffffffffu, *abort_flag)) return false;
             if (__any_sync(0xffffffffu, global_ns() - t0 > kWaitLimitNs)) {
                 *abort_flag = 1;
-                atomicOr(&st->error_flags, kErrTimeout);
+                if (st) atomicOr(&st->error_flags, kErrTimeout);
                 return false;
             }
         }

@@ -1,0 +1,215 @@
+// Products of 8-bit integers on the tensor cores (tcgen05, kind::i8): exact 32-bit sums in tensor memory, scaled in the epilogue.
+//
+// Rows of b (the weights' output channels) are the M side of the instruction and so the lanes of tensor memory, rows of a (tokens) its N side: a warp's
+// 32 lanes hold 32 neighbouring outputs of one token, and its stores are consecutive whatever the alignment of y.  Operands come by TMA as
+// 128-byte-swizzled K-major blocks of 128 values; what lies beyond k or the last row reads as zeros.
+//
+// k_product_tile: one tile of 128 channels x BN tokens per CTA, for few tokens or outputs.  Then the weights' bytes bound it, and what
+// counts is that all SMs stream: the K blocks of a tile are split over the CTAs of a cluster, which exchange their partial sums through
+// distributed shared memory (integers: in any order the same), each finishing its share of the tokens.
+//
+// Every wait on an mbarrier is bounded as in the emission kernels.  The call has no status to write to: a tile whose wait gave up is NaN.
+#pragma once
+#include "int8_product.cuh"
+#include "tcgen05.cuh"
+
+namespace cutoff {
+namespace layers {
+
+using namespace cutoff::async;
+using tc::elect_one;
+
+constexpr int kProdM = 128;                       // channels per tile: lanes of tensor memory
+constexpr int kProdK = 128;                       // values per K block: one 128-byte swizzle row
+constexpr int kProdABytes = kProdM * kProdK;
+
+// instruction descriptor: D = s32, A = B = s8, both K-major, N columns, M rows
+__host__ __device__ constexpr uint32_t instr_desc_s8(uint32_t n, uint32_t m) { return (2u << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | ((m >> 4) << 24); }
+
+__device__ __forceinline__ void umma_s8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// One result: the same steps in the same order in every kernel.
+__device__ __forceinline__ float scaled(int total, float a_scale, float b_scale, float bias) { return fmaf(static_cast<float>(total) * a_scale, b_scale, bias); }
+
+template <int BN>
+struct ProductTile {
+    static constexpr int kStageBytes = kProdABytes + BN * kProdK;
+    // Two CTAs per SM for few tokens, so that one streams while the other starts or ends.
+    static constexpr int kStages = BN <= 16 ? 5 : BN <= 32 ? 4 : BN <= 64 ? 3 : BN <= 128 ? 5 : 4;
+    static constexpr int kColumns = BN < 32 ? 32 : BN;                       // tensor memory comes in powers of two from 32
+    static constexpr int kThreads = 192;
+    static constexpr bool kOwnExchange = BN <= 64;                           // partial sums have room of their own, or reuse the ring
+    static constexpr int kExchangeBytes = kProdM * BN * 4;
+    static constexpr int kTailBytes = 256 + BN * 4;                          // barriers, flags; the tokens' scales
+    static_assert(kExchangeBytes <= kStages * kStageBytes || kOwnExchange, "exchange");
+    static constexpr size_t kSmemBytes = 1024 + kStages * kStageBytes + (kOwnExchange ? kExchangeBytes : 0) + kTailBytes;
+};
+
+// Grid: channel tiles x token tiles x splits, a cluster of `splits` CTAs per tile.
+template <typename T, int BN>
+__global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, ProductArgs p,
+                                                      int token_tiles, int splits) {
+    using Tile = ProductTile<BN>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u;
+    uint8_t* const base = smem_raw + (ring - raw);
+    int* const exchange = reinterpret_cast<int*>(base + (Tile::kOwnExchange ? Tile::kStages * Tile::kStageBytes : 0));
+    uint8_t* const tail = base + Tile::kStages * Tile::kStageBytes + (Tile::kOwnExchange ? Tile::kExchangeBytes : 0);
+    float* const token_scale = reinterpret_cast<float*>(tail + 256);
+    const uint32_t bars = smem_u32(tail);
+    const auto full = [&](int s) { return bars + 8 * s; };
+    const auto empty = [&](int s) { return bars + 8 * (Tile::kStages + s); };
+    const uint32_t acc_full = bars + 16 * Tile::kStages;
+    volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + 16 * Tile::kStages + 16);
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(tail + 16 * Tile::kStages + 24);
+    volatile int* const peer_failed = reinterpret_cast<volatile int*>(tail + 16 * Tile::kStages + 28);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int split = static_cast<int>(blockIdx.x) % splits, tile = static_cast<int>(blockIdx.x) / splits;
+    const int n0 = tile / token_tiles * kProdM;
+    const int64_t m0 = static_cast<int64_t>(tile % token_tiles) * BN;
+    const int blocks = ceil_div(p.k, kProdK);
+    const int first = static_cast<int>(static_cast<int64_t>(blocks) * split / splits), last = static_cast<int>(static_cast<int64_t>(blocks) * (split + 1) / splits);
+    DevState* const none = nullptr;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < Tile::kStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        mbar_init(acc_full, 1);
+        *abort_flag = 0;
+        *peer_failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))), "r"(Tile::kColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (splits > 1) tc::cluster_sync_all();       // the others' flags are set up before anything reaches across
+    tc::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    dependency_wait();                            // a is an earlier kernel's, perhaps
+
+    bool ok = true;
+    if (warp == 0) {
+        int s = 0;
+        uint32_t phase = 0;
+        int armed = 0;
+        for (int kb = first; ok && kb < last; ++kb) {
+            ok = mbar_wait(empty(s), phase ^ 1u, abort_flag, none);
+            if (!ok) break;
+            if (lane == 0) {
+                const uint32_t dst = ring + s * Tile::kStageBytes;
+                mbar_arrive_expect_tx(full(s), Tile::kStageBytes);
+                tc::tma_load_2d(dst, &map_b, kb * kProdK, n0, full(s));
+                tc::tma_load_2d(dst + kProdABytes, &map_a, kb * kProdK, static_cast<int>(m0), full(s));
+            }
+            __syncwarp();
+            armed = kb - first + 1;
+            if (++s == Tile::kStages) { s = 0; phase ^= 1u; }
+        }
+        // every copy has landed before the CTA leaves or its ring takes partial sums (if the products ran, all but the unread ones have)
+        if (!ok)
+            for (int b = armed > Tile::kStages ? armed - Tile::kStages : 0; b < armed; ++b) mbar_wait_quiet(full(b % Tile::kStages), (b / Tile::kStages) & 1u);
+    } else if (warp == 1) {
+        int s = 0;
+        uint32_t phase = 0;
+        for (int kb = first; ok && kb < last; ++kb) {
+            ok = mbar_wait(full(s), phase, abort_flag, none);
+            if (!ok) break;
+            tc::tc_fence_after();
+            if (elect_one()) {
+                const uint32_t at = ring + s * Tile::kStageBytes;
+                const uint64_t a_desc = tc::make_smem_desc(at), b_desc = tc::make_smem_desc(at + kProdABytes);
+#pragma unroll
+                for (int k = 0; k < kProdK / 32; ++k) umma_s8(tmem, a_desc + 2 * k, b_desc + 2 * k, instr_desc_s8(BN, kProdM), (kb - first) | k);
+                tc::umma_commit(empty(s));
+                if (kb == last - 1) tc::umma_commit(acc_full);
+            }
+            __syncwarp();
+            if (++s == Tile::kStages) { s = 0; phase ^= 1u; }
+        }
+        if (!ok) {
+            // no product is running when tensor memory is released (bounded)
+            if (elect_one()) tc::umma_commit(acc_full);
+            __syncwarp();
+            mbar_wait_quiet(acc_full, 0u);
+        }
+        __syncwarp();
+    } else {
+        for (int c = threadIdx.x - 64; c < BN; c += 128) token_scale[c] = m0 + c < p.m ? p.a_scale[m0 + c] : 0.f;
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        // a split of no K blocks adds nothing (its accumulator is never written)
+        if (last > first) ok = mbar_wait(acc_full, 0u, abort_flag, none);
+        tc::tc_fence_after();
+    }
+    const int quarter = warp & 3, channel = n0 + quarter * 32 + lane;
+    const bool epilogue = warp >= 2, has_channel = epilogue && channel < p.n;
+    const float b_scale = has_channel ? p.b_scale[channel] : 0.f, bias = has_channel && p.bias ? p.bias[channel] : 0.f;
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+    const auto put = [&](int c, float v) {
+        if (has_channel && m0 + c < p.m) from_float(static_cast<T*>(p.y)[(m0 + c) * p.y_ld + channel], v);
+    };
+    if (splits == 1) {
+        if (epilogue) {
+            const bool bad = !ok || *abort_flag;
+#pragma unroll 2
+            for (int c0 = 0; c0 < BN; c0 += 16) {
+                uint32_t r[16];
+                tc::tmem_ld16(lanes + c0, r);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) put(c0 + i, bad ? __int_as_float(0x7fc00000) : scaled(static_cast<int>(r[i]), token_scale[c0 + i], b_scale, bias));
+            }
+        }
+    } else {
+        if constexpr (!Tile::kOwnExchange) tc::cluster_sync_all();           // all CTAs are done with their rings
+        // token c of the tile belongs to CTA c / share, which has a place for every CTA's sums: [CTA][token][channel]
+        const int share = BN / splits;
+        if (epilogue) {
+            if (!ok || *abort_flag)
+                for (int r = 0; r < splits; ++r)
+                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(tc::map_to_cta(smem_u32(const_cast<int*>(peer_failed)), r)), "r"(1) : "memory");
+            for (int c0 = 0; c0 < BN; c0 += 16) {
+                uint32_t r[16];
+                tc::tmem_ld16(lanes + c0, r);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int c = c0 + i, owner = c / share;
+                    const uint32_t to = tc::map_to_cta(smem_u32(exchange + (split * share + c - owner * share) * kProdM + quarter * 32 + lane), owner);
+                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(last > first ? r[i] : 0u) : "memory");
+                }
+            }
+        }
+        tc::cluster_sync_all();
+        if (epilogue) {
+            const bool bad = *peer_failed;
+            for (int c = 0; c < share; ++c) {
+                int total = 0;
+                for (int r = 0; r < splits; ++r) total += exchange[(r * share + c) * kProdM + quarter * 32 + lane];
+                put(split * share + c, bad ? __int_as_float(0x7fc00000) : scaled(total, token_scale[split * share + c], b_scale, bias));
+            }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc::tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Tile::kColumns) : "memory");
+    }
+}
+
+}  // namespace layers
+}  // namespace cutoff

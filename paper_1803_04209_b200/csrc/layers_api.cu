@@ -9,6 +9,7 @@
 #include "dropout.cuh"
 #include "residual_norm.cuh"
 #include "int8_product.cuh"
+#include "int8_tc.cuh"
 
 using namespace cutoff;
 using namespace cutoff::layers;
@@ -108,14 +109,59 @@ GradPlan grad_plan(int64_t rows, int cols, int sms) {
 }
 
 // ---- products --------------------------------------------------------------------------------------------------------
+// Tensor map over int8 rows: boxes of box_rows rows x 128 bytes, 128-byte swizzle.  The driver entry point is looked up once.
+bool make_byte_map(CUtensorMap* map, const int8_t* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+    typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const EncodeFn encode = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
+        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeFn>(fn) : nullptr;
+    }();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld)};
+    const cuuint32_t box[2] = {kProdK, static_cast<cuuint32_t>(box_rows)};
+    const cuuint32_t elem[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int BN>
+bool launch_product_tile(const ProductArgs& p, int device, cudaStream_t s) {
+    using Tile = ProductTile<BN>;
+    CUtensorMap map_a, map_b;
+    if (!make_byte_map(&map_a, p.a, p.m, p.k, p.a_ld, BN) || !make_byte_map(&map_b, p.b, p.n, p.k, p.b_ld, kProdM)) return false;
+    if (cudaFuncSetAttribute(k_product_tile<T, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Tile::kSmemBytes)) != cudaSuccess) return false;
+    const int64_t token_tiles = ceil_div64(p.m, BN), tiles = token_tiles * ceil_div(p.n, kProdM);
+    // K blocks of a tile are split until the GPU is filled, but no CTA gets less than two of them
+    const int sms = sm_count(device), blocks = ceil_div(p.k, kProdK), want = BN <= 64 ? sms * 3 / 2 : sms * 3 / 4;
+    int splits = 1;
+    while (splits < 8 && tiles * splits < want && blocks >= 4 * splits) splits *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(tiles * splits));
+    cfg.blockDim = dim3(Tile::kThreads);
+    cfg.dynamicSmemBytes = Tile::kSmemBytes;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = splits;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, k_product_tile<T, BN>, map_b, map_a, p, static_cast<int>(token_tiles), splits) == cudaSuccess;
+}
+
 template <typename T>
-void launch_product(const ProductArgs& p, cudaStream_t s) {
-    const auto run = [&](auto rows) {
-        constexpr int MT = decltype(rows)::value;
-        launch_dependent(k_product_dot<T, MT>, dim3(ceil_div(p.n, kDotWarps), static_cast<unsigned>(ceil_div64(p.m, MT))), dim3(kDotWarps * 32), 0, s, p);
-    };
-    if (p.m == 1) run(std::integral_constant<int, 1>{});
-    else run(std::integral_constant<int, 8>{});
+bool launch_product(const ProductArgs& p, int device, cudaStream_t s) {
+    if (p.m <= 16) return launch_product_tile<T, 16>(p, device, s);
+    if (p.m <= 32) return launch_product_tile<T, 32>(p, device, s);
+    if (p.m <= 64) return launch_product_tile<T, 64>(p, device, s);
+    if (p.m <= 128 || ceil_div64(p.m, 128) * ceil_div(p.n, kProdM) <= sm_count(device)) return launch_product_tile<T, 128>(p, device, s);
+    return launch_product_tile<T, 256>(p, device, s);
 }
 
 }  // namespace
@@ -243,8 +289,9 @@ int cutoff_quantized_product(int device, int64_t m, int32_t n, int32_t k, const 
     DeviceGuard guard(device);
     if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
     const ProductArgs p{a, b, a_scale, b_scale, bias, y, m, a_ld, b_ld, y_ld, n, k};
-    with_type(type, [&](auto t) { launch_product<decltype(t)>(p, static_cast<cudaStream_t>(stream)); });
-    return status();
+    bool ok = false;
+    with_type(type, [&](auto t) { ok = launch_product<decltype(t)>(p, device, static_cast<cudaStream_t>(stream)); });
+    return ok ? status() : CUTOFF_ERR_CUDA;
 }
 
 }  // extern "C"
