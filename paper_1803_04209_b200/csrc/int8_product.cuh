@@ -24,7 +24,7 @@ constexpr int kQuantizeThreads = 256;
 // A CTA per row.  The row is read twice; the second time it is in the L1 or L2.
 template <typename T, int V>
 __global__ void __launch_bounds__(kQuantizeThreads) k_quantize_rows(QuantizeArgs a) {
-    __shared__ float scratch[2 * 32 * Team<0>::kMostSums];
+    __shared__ __align__(16) float scratch[Team<0>::kScratch];
     Team<0> team(scratch);
     const T* const x = static_cast<const T*>(a.x) + blockIdx.x * a.x_ld;
     int8_t* const q = a.q + blockIdx.x * a.q_ld;

@@ -103,10 +103,16 @@ __device__ __forceinline__ void load_params(const float* p, int c, float other, 
 // depends on nothing but the number of threads, and every thread gets the same bits.
 template <int SIZE>
 struct Team {
-    static constexpr int kMostSums = 5;
-    float* scratch;                 // CTA: [2][32][kMostSums]
+    static constexpr int kMostSums = 2;
+    static constexpr int kScratch = 2 * kMostSums * 32;
+    float* scratch;                 // CTA: [2][kMostSums][32 warps], 16-byte aligned
     uint32_t parity = 0;
-    __device__ __forceinline__ explicit Team(float* s) : scratch(s) {}
+    __device__ __forceinline__ explicit Team(float* s) : scratch(s) {
+        if constexpr (SIZE == 0) {
+            for (int i = threadIdx.x; i < kScratch; i += blockDim.x) s[i] = 0.f;
+            __syncthreads();
+        }
+    }
     __device__ __forceinline__ int size() const { return SIZE ? SIZE : blockDim.x; }
     __device__ __forceinline__ int rank() const { return SIZE ? threadIdx.x % SIZE : threadIdx.x; }
 
@@ -119,25 +125,24 @@ struct Team {
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
         if constexpr (SIZE == 0) {
-            const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+            const int warps = blockDim.x >> 5;
             if (warps == 1) return;
             float* const s = scratch + parity * 32 * kMostSums;     // the other half may still be read: one barrier is enough
             parity ^= 1u;
-            if (lane < N) {
-                float mine = v[0];
+            if ((threadIdx.x & 31) == 0)
 #pragma unroll
-                for (int i = 1; i < N; ++i) mine = lane == i ? v[i] : mine;
-                s[warp * kMostSums + lane] = mine;
-            }
+                for (int i = 0; i < N; ++i) s[32 * i + (threadIdx.x >> 5)] = v[i];
             __syncthreads();
+            // every thread adds all warps' sums, four at a time; what belongs to no warp is zero
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = lane < warps ? s[lane * kMostSums + i] : 0.f;
-            for (int d = warps > 16 ? 16 : warps > 8 ? 8 : warps > 4 ? 4 : warps > 2 ? 2 : 1; d; d >>= 1)
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
-            // lanes beyond the power of two hold other sums when warps is no power of two: lane 0's is the whole one
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
+            for (int i = 0; i < N; ++i) {
+                float4 q = *reinterpret_cast<const float4*>(s + 32 * i);
+                for (int w = 4; w < warps; w += 4) {
+                    const float4 t = *reinterpret_cast<const float4*>(s + 32 * i + w);
+                    q.x += t.x; q.y += t.y; q.z += t.z; q.w += t.w;
+                }
+                v[i] = (q.x + q.y) + (q.z + q.w);
+            }
         }
     }
     // The largest of the teams' values, which are compared as unsigned integers.
@@ -150,9 +155,9 @@ struct Team {
             if (warps == 1) return v;
             uint32_t* const s = reinterpret_cast<uint32_t*>(scratch) + parity * 32 * kMostSums;
             parity ^= 1u;
-            if (lane == 0) s[warp * kMostSums] = v;
+            if (lane == 0) s[warp] = v;
             __syncthreads();
-            v = __reduce_max_sync(0xffffffffu, lane < warps ? s[lane * kMostSums] : 0u);
+            v = __reduce_max_sync(0xffffffffu, lane < warps ? s[lane] : 0u);
         }
         return v;
     }

@@ -85,7 +85,8 @@ NormArgs norm_args(const cutoff_norm_layer* l) {
     NormArgs a{};
     a.x = l->x; a.h = l->h; a.gate = l->gate;
     a.scale = l->scale; a.post_w = l->post_weight; a.post_b = l->post_bias; a.pre_w = l->pre_weight; a.pre_b = l->pre_bias;
-    a.rows = l->rows; a.x_ld = l->x_ld; a.h_ld = l->h_ld; a.gate_ld = l->gate_ld; a.gate_rows = l->gate_rows;
+    a.rows = static_cast<int>(l->rows); a.x_ld = l->x_ld; a.h_ld = l->h_ld; a.gate_ld = l->gate_ld;
+    a.gate_rows = !l->gate ? 1 : static_cast<int>(l->gate_rows < INT32_MAX ? l->gate_rows : INT32_MAX);
     a.cols = l->cols; a.gate_kind = l->gate_kind; a.post = l->post; a.pre = l->pre;
     a.eps = l->eps; a.inv_cols = 1.f / static_cast<float>(l->cols);
     return a;
@@ -95,17 +96,6 @@ bool whole_packs(const cutoff_norm_layer* l) {
     return l->cols * size % 16 == 0 && rows_aligned(l->x, l->x_ld, size, 16) && rows_aligned(l->h, l->h_ld, size, 16) &&
            rows_aligned(l->gate, l->gate_ld, size, 16) && aligned16(l->scale) && aligned16(l->post_weight) && aligned16(l->post_bias) &&
            aligned16(l->pre_weight) && aligned16(l->pre_bias);
-}
-
-// Teams of the backward pass: as many as are resident, but so that none adds more than kMostTeamRows rows in a row.
-constexpr int64_t kMostTeamRows = 1024;
-GradPlan grad_plan(int64_t rows, int cols, int sms) {
-    const int per_cta = cols <= 32 ? kNormWarpThreads / 4 : cols <= 128 ? kNormWarpThreads / 16 : cols <= 512 ? kNormWarpThreads / 32 : 1;
-    int64_t ctas = static_cast<int64_t>(sms) * (cols <= 512 ? 2 : 2);
-    const int64_t few = ceil_div64(rows, per_cta), many = ceil_div64(rows, kMostTeamRows * per_cta);
-    ctas = ctas < many ? many : ctas;
-    ctas = ctas < few ? ctas : few;
-    return GradPlan{ctas, ctas * per_cta};
 }
 
 // ---- products --------------------------------------------------------------------------------------------------------
@@ -210,17 +200,21 @@ int cutoff_residual_norm(int device, const cutoff_norm_layer* layer, void* resid
     const int size = type_size(layer->type);
     const bool packs = whole_packs(layer) && rows_aligned(residual, residual_ld, size, 16) &&
                        (norm_scale ? rows_aligned(norm, norm_ld, 1, 16 / size) : rows_aligned(norm, norm_ld, size, 16));
-    with_type(layer->type, [&](auto t) {
-        using T = decltype(t);
-        run_norm<T>(a, packs, static_cast<cudaStream_t>(stream));
-    });
-    return status();
+    bool ok = false;
+    with_type(layer->type, [&](auto t) { ok = run_norm<decltype(t)>(a, packs, sm_count(device), static_cast<cudaStream_t>(stream)); });
+    return ok ? status() : CUTOFF_ERR_CUDA;
 }
 
 int64_t cutoff_residual_norm_grad_workspace_bytes(int64_t rows, int32_t cols) {
     if (rows < 0 || rows > INT32_MAX || cols < 1 || cols > kMostCols) return CUTOFF_ERR_BAD_ARG;
-    const GradPlan plan = grad_plan(rows, cols, 256);        // for a GPU of up to 256 SMs
-    return (4 * plan.ctas + 2 * plan.teams) * cols * static_cast<int64_t>(sizeof(float)) + 256;
+    // the larger of what the two ways to lay out the teams take
+    int64_t most = 0;
+    for (const bool many_sums : {false, true}) {
+        const GradPlan plan = grad_plan(static_cast<int>(rows), cols, many_sums, kMostSms);
+        const int64_t floats = (4 * static_cast<int64_t>(plan.ctas) + 2 * static_cast<int64_t>(plan.teams)) * cols;
+        most = floats > most ? floats : most;
+    }
+    return most * static_cast<int64_t>(sizeof(float)) + 256;
 }
 
 int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const void* d_residual, int64_t d_residual_ld, const void* d_norm,
@@ -238,17 +232,17 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
     if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int sms = sm_count(device);
-    const GradPlan plan = grad_plan(layer->rows, layer->cols, sms < 256 ? sms : 256);
     const bool bias = layer->post_bias || layer->pre_bias, groups = layer->gate && layer->gate_rows > 1;
+    const GradPlan plan = grad_plan(static_cast<int>(layer->rows), layer->cols, bias || groups, sms);
     NormFinishArgs q{};
     NormGradArgs& g = q.g;
     g.f = norm_args(layer);
     g.d_r = d_residual; g.d_n = d_norm; g.d_r_ld = d_residual_ld; g.d_n_ld = d_norm_ld;
     g.d_x = grads->x; g.d_h = grads->h; g.d_gate = grads->gate; g.d_x_ld = grads->x_ld; g.d_h_ld = grads->h_ld; g.d_gate_ld = grads->gate_ld;
     g.sums = static_cast<float*>(workspace);
-    g.gate_sums = g.sums + 4 * plan.ctas * layer->cols;
+    g.gate_sums = g.sums + 4 * static_cast<int64_t>(plan.ctas) * layer->cols;
     g.teams = plan.teams;
-    q.ctas = static_cast<int>(plan.ctas); q.each = bias ? 4 : 2;
+    q.ctas = plan.ctas; q.each = bias ? 4 : 2;
     q.d_scale = grads->scale; q.d_post_w = grads->post_weight; q.d_post_b = grads->post_bias; q.d_pre_w = grads->pre_weight; q.d_pre_b = grads->pre_bias;
     const int size = type_size(layer->type);
     const bool packs = whole_packs(layer) && rows_aligned(d_residual, d_residual_ld, size, 16) && rows_aligned(d_norm, d_norm_ld, size, 16) &&
@@ -256,8 +250,10 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
                        rows_aligned(grads->gate, grads->gate_ld, size, 16);
     const bool sums = grads->scale || grads->post_weight || grads->post_bias || grads->pre_weight || grads->pre_bias;
     q.column_blocks = sums ? ceil_div(layer->cols, kFinishColumns) : 0;
-    const int gate_blocks = groups && grads->gate && layer->rows > 0 ? static_cast<int>(plan.teams < 2 * sms ? plan.teams : 2 * sms) : 0;
-    with_type(layer->type, [&](auto t) { run_norm_grad<decltype(t)>(q, plan, packs, bias, groups, q.column_blocks + gate_blocks, s); });
+    const int gate_blocks = groups && grads->gate && layer->rows > 0 ? plan.teams < 2 * sms ? plan.teams : 2 * sms : 0;
+    bool ok = false;
+    with_type(layer->type, [&](auto t) { ok = run_norm_grad<decltype(t)>(q, plan, packs, bias, groups, q.column_blocks + gate_blocks, s); });
+    if (!ok) return CUTOFF_ERR_CUDA;
     return status();
 }
 

@@ -3,7 +3,7 @@
 
 namespace cutoff {
 namespace layers {
-template void run_norm<__nv_bfloat16>(const NormArgs&, bool, cudaStream_t);
-template void run_norm_grad<__nv_bfloat16>(const NormFinishArgs&, const GradPlan&, bool, bool, bool, int, cudaStream_t);
+template bool run_norm<__nv_bfloat16>(const NormArgs&, bool, int, cudaStream_t);
+template bool run_norm_grad<__nv_bfloat16>(NormFinishArgs&, const GradPlan&, bool, bool, bool, int, cudaStream_t);
 }  // namespace layers
 }  // namespace cutoff

@@ -3,7 +3,7 @@
 
 namespace cutoff {
 namespace layers {
-template void run_norm<__half>(const NormArgs&, bool, cudaStream_t);
-template void run_norm_grad<__half>(const NormFinishArgs&, const GradPlan&, bool, bool, bool, int, cudaStream_t);
+template bool run_norm<__half>(const NormArgs&, bool, int, cudaStream_t);
+template bool run_norm_grad<__half>(NormFinishArgs&, const GradPlan&, bool, bool, bool, int, cudaStream_t);
 }  // namespace layers
 }  // namespace cutoff

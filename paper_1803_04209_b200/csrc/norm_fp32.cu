@@ -3,7 +3,7 @@
 
 namespace cutoff {
 namespace layers {
-template void run_norm<float>(const NormArgs&, bool, cudaStream_t);
-template void run_norm_grad<float>(const NormFinishArgs&, const GradPlan&, bool, bool, bool, int, cudaStream_t);
+template bool run_norm<float>(const NormArgs&, bool, int, cudaStream_t);
+template bool run_norm_grad<float>(NormFinishArgs&, const GradPlan&, bool, bool, bool, int, cudaStream_t);
 }  // namespace layers
 }  // namespace cutoff
