@@ -7,6 +7,9 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
+#include "async.cuh"
 #include "common.cuh"
 
 namespace cutoff {
@@ -82,20 +85,135 @@ __device__ __forceinline__ void store_pack(T* p, const float (&f)[V]) {
     }
 }
 
-// V parameters (fp32, used by every row) from column c on; `other` where there are none.
+// ---- one fp32 value, or two that one instruction works on (V > 1): the kernels' arithmetic is half their instructions
+struct F1 {
+    float v;
+};
+struct F2 {
+    unsigned long long v;
+};
 template <int V>
-__device__ __forceinline__ void load_params(const float* p, int c, float other, float (&f)[V]) {
-    if (p == nullptr) {
+using Num = typename std::conditional<V == 1, F1, F2>::type;
+template <int V>
+constexpr int kNums = V == 1 ? 1 : V / 2;
+
+__device__ __forceinline__ F1 mul(F1 a, F1 b) { return F1{a.v * b.v}; }
+__device__ __forceinline__ F1 add(F1 a, F1 b) { return F1{a.v + b.v}; }
+__device__ __forceinline__ F1 fma(F1 a, F1 b, F1 c) { return F1{fmaf(a.v, b.v, c.v)}; }
+__device__ __forceinline__ float total(F1 a) { return a.v; }
+__device__ __forceinline__ F2 mul(F2 a, F2 b) { return F2{mul2(a.v, b.v)}; }
+__device__ __forceinline__ F2 add(F2 a, F2 b) { return F2{add2(a.v, b.v)}; }
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
+    fma2(c.v, a.v, b.v);
+    return c;
+}
+__device__ __forceinline__ float total(F2 a) {
+    float x, y;
+    unpack2(a.v, x, y);
+    return x + y;
+}
+template <typename N>
+__device__ __forceinline__ N splat(float x) {
+    if constexpr (std::is_same<N, F1>::value) return F1{x};
+    else return F2{pack2(x, x)};
+}
+// f applied to each value
+template <typename F>
+__device__ __forceinline__ F1 each(F1 a, F f) { return F1{f(a.v)}; }
+template <typename F>
+__device__ __forceinline__ F2 each(F2 a, F f) {
+    float x, y;
+    unpack2(a.v, x, y);
+    return F2{pack2(f(x), f(y))};
+}
+
+template <typename T>
+__device__ __forceinline__ F2 pair_of(uint32_t w) {
+    if constexpr (std::is_same<T, __half>::value) {
+        const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        return F2{pack2(t.x, t.y)};
+    } else {
+        return F2{pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u))};
+    }
+}
+// V values of type T at a shared-memory address (16-byte aligned if V > 1), or zeros.  Predicates and not branches, here and in write_global: a
+// branch for each pack costs more than the pack's arithmetic.
+template <typename T, int V>
+__device__ __forceinline__ void read_shared(uint32_t at, bool ok, Num<V> (&f)[kNums<V>]) {
+    const int p = ok;
+    if constexpr (V == 1 && sizeof(T) == 4) {
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\tmov.f32 %0, 0f00000000;\n\t@p ld.shared.f32 %0, [%1];\n\t}" : "=f"(f[0].v) : "r"(at), "r"(p) : "memory");
+    } else if constexpr (V == 1) {
+        unsigned short u;
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\tmov.u16 %0, 0;\n\t@p ld.shared.u16 %0, [%1];\n\t}" : "=h"(u) : "r"(at), "r"(p) : "memory");
+        f[0].v = to_float(*reinterpret_cast<const T*>(&u));
+    } else if constexpr (sizeof(T) == 4) {
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %3, 0;\n\tmov.b64 %0, 0;\n\tmov.b64 %1, 0;\n\t@p ld.shared.v2.b64 {%0, %1}, [%2];\n\t}"
+                     : "=l"(f[0].v), "=l"(f[1].v) : "r"(at), "r"(p) : "memory");
+    } else {
+        uint32_t w[4];
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t@p ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at), "r"(p) : "memory");
 #pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = other;
-    } else if constexpr (V % 4 == 0) {
+        for (int i = 0; i < 4; ++i) f[i] = pair_of<T>(w[i]);
+    }
+}
+// V fp32 values at a shared-memory address
+template <int V>
+__device__ __forceinline__ void read_shared_params(uint32_t at, Num<V> (&f)[kNums<V>]) {
+    if constexpr (V == 1) {
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[0].v) : "r"(at) : "memory");
+    } else {
 #pragma unroll
-        for (int i = 0; i < V; i += 4) {
-            const float4 t = __ldg(reinterpret_cast<const float4*>(p + c + i));
-            f[i] = t.x; f[i + 1] = t.y; f[i + 2] = t.z; f[i + 3] = t.w;
+        for (int i = 0; i < V / 2; i += 2) asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f[i].v), "=l"(f[i + 1].v) : "r"(at + 8 * i) : "memory");
+    }
+}
+// V values of type T in global memory that other rows use too
+template <typename T, int V>
+__device__ __forceinline__ void read_global(const T* p, Num<V> (&f)[kNums<V>]) {
+    if constexpr (V == 1) {
+        f[0].v = to_float(*p);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < V / 2; i += 2) {
+            const ulonglong2 t = __ldg(reinterpret_cast<const ulonglong2*>(p + 2 * i));
+            f[i].v = t.x;
+            f[i + 1].v = t.y;
         }
     } else {
-        f[0] = __ldg(p + c);
+        const uint4 t = __ldg(reinterpret_cast<const uint4*>(p));
+        f[0] = pair_of<T>(t.x); f[1] = pair_of<T>(t.y); f[2] = pair_of<T>(t.z); f[3] = pair_of<T>(t.w);
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void write_global(T* at, bool ok, const Num<V> (&n)[kNums<V>]) {
+    const int p = ok;
+    if constexpr (V == 1) {
+        T v;
+        from_float(v, n[0].v);
+        if constexpr (sizeof(T) == 4) {
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p st.global.f32 [%0], %1;\n\t}" ::"l"(at), "f"(n[0].v), "r"(p) : "memory");
+        } else {
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p st.global.u16 [%0], %1;\n\t}" ::"l"(at), "h"(*reinterpret_cast<const unsigned short*>(&v)), "r"(p) : "memory");
+        }
+    } else if constexpr (sizeof(T) == 4) {
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %3, 0;\n\t@p st.global.v2.b64 [%0], {%1, %2};\n\t}" ::"l"(at), "l"(n[0].v), "l"(n[1].v), "r"(p) : "memory");
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x, y;
+            unpack2(n[i].v, x, y);
+            if constexpr (std::is_same<T, __half>::value) {
+                const __half2 h = __floats2half2_rn(x, y);
+                w[i] = *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+                w[i] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+        }
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %5, 0;\n\t@p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n\t}"
+                     ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(p) : "memory");
     }
 }
 
@@ -114,6 +232,10 @@ struct Team {
         }
     }
     __device__ __forceinline__ int size() const { return SIZE ? SIZE : blockDim.x; }
+    __device__ __forceinline__ void sync() const {
+        if constexpr (SIZE == 0) __syncthreads();
+        else __syncwarp();
+    }
     __device__ __forceinline__ int rank() const { return SIZE ? threadIdx.x % SIZE : threadIdx.x; }
 
     template <int N>
@@ -162,6 +284,73 @@ struct Team {
         return v;
     }
 };
+
+// ---- rows on their way to shared memory -------------------------------------------------------------------------------
+// An operand whose rows are staged.
+struct RowOperand {
+    const char* at;
+    int64_t ld;                     // bytes from one row to the next
+};
+constexpr int kMostOperands = 5;
+struct RowOperands {
+    RowOperand o[kMostOperands];
+    int n;
+    int row_bytes;
+    int slot_bytes;                 // of shared memory for a row of an operand: a multiple of 16
+    int stages;                     // rows of a team in shared memory: 2, the next one on its way, or 1
+};
+
+// The rows of a team, copied by the asynchronous copy engine: one thread asks for a whole row of each operand and no thread of the team spends
+// an instruction on it.  Copies are whole 16-byte units, rounded outwards where a row does not start or end on one.  Every wait is
+// bounded; a row whose copies do not arrive in time is marked by the caller.
+template <typename T, int SIZE>
+struct RowPipe {
+    const RowOperands& r;
+    uint32_t slots, bars;           // this team's
+    __device__ __forceinline__ RowPipe(const RowOperands& operands, uint32_t smem, uint32_t barriers, int team)
+        : r(operands), slots(smem + team * operands.stages * operands.n * operands.slot_bytes), bars(barriers + 16 * team) {}
+    // One thread of the team, before the first use (and a barrier of the CTA in between).
+    __device__ __forceinline__ void open() const {
+        async::mbar_init(bars, r.n);
+        async::mbar_init(bars + 8, r.n);
+        async::fence_barrier_init();
+    }
+    __device__ __forceinline__ uint32_t slot(int stage, int o) const { return slots + (stage * r.n + o) * r.slot_bytes; }
+    // The team's first threads, an operand each; all of the team is done with what the stage held.
+    __device__ __forceinline__ void fetch(int stage, int64_t row, const Team<SIZE>& team) const {
+        for (int o = team.rank(); o < r.n; o += team.size()) {
+            const char* const p = r.o[o].at + row * r.o[o].ld;
+            const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u, bytes = (off + r.row_bytes + 15u) & ~15u;
+            async::mbar_arrive_expect_tx(bars + 8 * stage, bytes);
+            async::bulk_load_1d(slot(stage, o), p - off, bytes, bars + 8 * stage);
+        }
+    }
+    // Turn t of the team; false if the copies have not arrived within the limit.
+    __device__ __forceinline__ bool wait(int turn) const {
+        const int stage = r.stages == 2 ? turn & 1 : 0;
+        const uint32_t bar = bars + 8 * stage, parity = (r.stages == 2 ? turn >> 1 : turn) & 1;
+        if (async::mbar_try_wait(bar, parity)) return true;
+        const unsigned long long t0 = async::global_ns();
+        while (!async::mbar_try_wait(bar, parity))
+            if (async::global_ns() - t0 > async::kWaitLimitNs) return false;
+        return true;
+    }
+    // After a wait that gave up: the copies in flight land before the CTA leaves (bounded again).
+    __device__ __forceinline__ void drain() const {
+        for (int i = 0; i < 2 * r.stages; ++i) async::mbar_wait_quiet(bars + 8 * (i >> 1), i & 1);
+    }
+    // Address of the row's first value (V > 1: it is aligned).
+    template <int V>
+    __device__ __forceinline__ uint32_t row_at(int stage, int o, int64_t row) const {
+        const uint32_t s = slot(stage, o);
+        if constexpr (V > 1) return s;
+        else return s + (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(r.o[o].at + row * r.o[o].ld)) & 15u);
+    }
+};
+// Bytes of a slot: whole packs of all threads, so that what lies beyond the row can be zeros; single values: the row and what rounding adds.
+__host__ __device__ inline int slot_bytes_of(int row_bytes, int team_threads, int per_thread, int size, bool packs) {
+    return packs ? team_threads * per_thread * size : (row_bytes + 30 + 15) / 16 * 16;
+}
 
 // 8-bit integers of a row whose largest magnitude has these bits (compared as an integer, so that a NaN is the largest of all): value =
 // integer * scale, integer = rint(value * inverse).  A row of magnitudes below 2^-100 counts as zeros, because 127 / top would leave the range;

@@ -207,10 +207,10 @@ int cutoff_residual_norm(int device, const cutoff_norm_layer* layer, void* resid
 
 int64_t cutoff_residual_norm_grad_workspace_bytes(int64_t rows, int32_t cols) {
     if (rows < 0 || rows > INT32_MAX || cols < 1 || cols > kMostCols) return CUTOFF_ERR_BAD_ARG;
-    // the larger of what the two ways to lay out the teams take
+    // the largest of what the ways to lay out the teams take
     int64_t most = 0;
-    for (const bool many_sums : {false, true}) {
-        const GradPlan plan = grad_plan(static_cast<int>(rows), cols, many_sums, kMostSms);
+    for (const int way : {0, 1, 2}) {
+        const GradPlan plan = grad_plan(static_cast<int>(rows), cols, way == 2 ? 4 : 2, way == 1, kMostSms);
         const int64_t floats = (4 * static_cast<int64_t>(plan.ctas) + 2 * static_cast<int64_t>(plan.teams)) * cols;
         most = floats > most ? floats : most;
     }
@@ -233,7 +233,7 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int sms = sm_count(device);
     const bool bias = layer->post_bias || layer->pre_bias, groups = layer->gate && layer->gate_rows > 1;
-    const GradPlan plan = grad_plan(static_cast<int>(layer->rows), layer->cols, bias || groups, sms);
+    const GradPlan plan = grad_plan(static_cast<int>(layer->rows), layer->cols, type_size(layer->type), bias || groups, sms);
     NormFinishArgs q{};
     NormGradArgs& g = q.g;
     g.f = norm_args(layer);

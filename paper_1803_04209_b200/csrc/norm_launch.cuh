@@ -25,26 +25,45 @@ void with_team(int cols, bool wide, F f) {
 inline int team_threads(int cols, int per_thread) { return ceil_div(ceil_div(cols, per_thread), 32) * 32; }
 
 // Most bytes of shared memory that the CTAs of an SM may take together for their operands.
-constexpr int kNormSmem = 220 * 1024;
+constexpr int kNormSmem = 228 * 1024;
+
+// CTAs of an SM and rows of a team in shared memory: `most` CTAs by their registers; two stages unless they do not fit even one CTA.
+struct Staging {
+    int per_sm, stages, bytes;
+};
+inline Staging staging(int most, int stage_bytes, int more_bytes) {
+    constexpr int kFixed = 2560;                  // what the system and static arrays take of a CTA, at most
+    Staging s{most, 2, 0};
+    while (s.per_sm > 1 && s.per_sm * (2 * stage_bytes + more_bytes + kFixed) > kNormSmem) --s.per_sm;
+    if (2 * stage_bytes + more_bytes + kFixed > kNormSmem) s.stages = 1;
+    s.bytes = s.stages * stage_bytes + more_bytes;
+    return s;
+}
 
 template <typename T, int V>
 bool launch_norm(const NormArgs& a, int sms, cudaStream_t s) {
     bool ok = false;
-    with_team<T, V>(a.cols, a.rows > 512, [&](auto v, auto k, auto size) {
-        constexpr int VV = decltype(v)::value, K = decltype(k)::value, SIZE = decltype(size)::value;
-        const auto kernel = k_residual_norm<T, VV, K, SIZE>;
-        const int threads = SIZE ? kNormWarpThreads : team_threads(a.cols, VV * K), teams = SIZE ? kNormWarpThreads / (SIZE ? SIZE : 1) : 1;
-        const int stage = norm_operands(a) * K * threads * static_cast<int>(sizeof(Pack<T, VV>));
-        // as many CTAs as fit the registers (64 for each of 1024 threads), two rows of each in shared memory, or one
-        int per_sm = 1024 / threads, stages = 2;
-        if (per_sm > 16) per_sm = 16;
-        while (per_sm > 1 && per_sm * (2 * stage + 2048) > kNormSmem) --per_sm;
-        if (2 * stage + 2048 > kNormSmem) stages = 1;
-        const int ctas = ceil_div(a.rows, teams), resident = sms * per_sm;
-        if (ctas <= resident) stages = 1;         // a row each
-        const int smem = stages * stage;
-        if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return;
-        kernel<<<ctas < resident ? ctas : resident, threads, smem, s>>>(a, stages);
+    with_team<T, V>(a.cols, a.rows > 512 || a.cols > 4096, [&](auto v, auto k, auto size) {
+        constexpr int VV = decltype(v)::value, K = decltype(k)::value, SIZE = decltype(size)::value, kSize = static_cast<int>(sizeof(T));
+        const bool layer = a.post == kNormLayer || a.pre == kNormLayer;
+        const bool bias = a.post_b || a.pre_b;
+        const auto kernel = layer && bias ? k_residual_norm<T, VV, K, SIZE, true, true> : layer ? k_residual_norm<T, VV, K, SIZE, true, false>
+                            : bias ? k_residual_norm<T, VV, K, SIZE, false, true> : k_residual_norm<T, VV, K, SIZE, false, false>;
+        const int threads = SIZE ? kNormWarpThreads : team_threads(a.cols, VV * K);
+        RowOperands ops{};
+        const auto use = [&](const void* p, int64_t ld) { ops.o[ops.n++] = RowOperand{static_cast<const char*>(p), ld * kSize}; };
+        use(a.x, a.x_ld);
+        if (a.h) use(a.h, a.h_ld);
+        if (a.gate && a.gate_rows == 1) use(a.gate, a.gate_ld);
+        ops.row_bytes = a.cols * kSize;
+        ops.slot_bytes = slot_bytes_of(ops.row_bytes, SIZE ? SIZE : threads, VV * K, kSize, VV > 1);
+        const int stage = kTeamsHere<SIZE> * ops.n * ops.slot_bytes, by_registers = 65536 / (threads * (bias ? kNormRegisters<VV, K, true> : kNormRegisters<VV, K, false>)), most = by_registers < 16 ? by_registers : 16;
+        const int ctas = ceil_div(a.rows, kTeamsHere<SIZE>);
+        Staging st = staging(most, stage, 0);
+        if (ctas <= sms * st.per_sm) st.stages = 1, st.bytes = stage;         // a row each
+        ops.stages = st.stages;
+        if (st.bytes > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, st.bytes) != cudaSuccess) return;
+        kernel<<<ctas < sms * st.per_sm ? ctas : sms * st.per_sm, threads, st.bytes, s>>>(a, ops);
         ok = true;
     });
     return ok;
@@ -55,15 +74,35 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
     NormGradArgs& g = q.g;
     bool ok = false;
     const auto run = [&](auto k, auto size) {
-        constexpr int K = decltype(k)::value, SIZE = decltype(size)::value;
-        const auto kernel = k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS>;
-        const size_t stage = static_cast<size_t>(grad_operands<GROUPS>(g)) * K * plan.threads * sizeof(Pack<T, V>);
-        g.stages = 2 * stage + 2048 <= kNormSmem ? 2 : 1;
-        size_t smem = g.stages * stage;
-        const size_t sums = SIZE ? g.f.cols * sizeof(float) : 0;
-        if (smem < sums) smem = sums;
-        if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return;
-        kernel<<<plan.ctas, plan.threads, smem, s>>>(g);
+        constexpr int K = decltype(k)::value, SIZE = decltype(size)::value, kSize = static_cast<int>(sizeof(T));
+        RowOperands ops{};
+        const auto use = [&](const void* p, int64_t ld) {
+            if (p) ops.o[ops.n++] = RowOperand{static_cast<const char*>(p), ld * kSize};
+        };
+        use(g.f.x, g.f.x_ld);
+        use(g.f.h, g.f.h_ld);
+        if (!GROUPS) use(g.f.gate, g.f.gate_ld);
+        use(g.d_r, g.d_r_ld);
+        use(g.d_n, g.d_n_ld);
+        ops.row_bytes = g.f.cols * kSize;
+        ops.slot_bytes = slot_bytes_of(ops.row_bytes, SIZE ? SIZE : plan.threads, V * K, kSize, V > 1);
+        const int stage = kTeamsHere<SIZE> * ops.n * ops.slot_bytes,
+                  params = (BIAS ? 3 : 2) * 4 * (SIZE ? SIZE : plan.threads) * V * K;
+        // the plan's CTAs are resident by their registers; where shared memory holds fewer, the others follow
+        Staging st = staging(plan.per_sm, stage, params);
+        const bool layer = g.f.post == kNormLayer || g.f.pre == kNormLayer;
+        auto kernel = layer ? k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, true, true> : k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, false, true>;
+        if constexpr (sizeof(T) == 4 && V * K == 16 && SIZE == 0)
+            if (st.bytes > 225 * 1024) {
+                st.bytes -= params;
+                kernel = layer ? k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, true, false> : k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, false, false>;
+            }
+        ops.stages = st.stages;
+        g.param_bytes = st.stages * stage;
+        const int sums = SIZE ? g.f.cols * 4 : 0;
+        if (st.bytes < sums) st.bytes = sums;
+        if (st.bytes > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, st.bytes) != cudaSuccess) return;
+        kernel<<<plan.ctas, plan.threads, st.bytes, s>>>(g, ops);
         ok = true;
     };
     using std::integral_constant;
@@ -75,7 +114,7 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
     else if (plan.lanes == 32) {
         if constexpr (!BIAS && !GROUPS) run(sixteen, integral_constant<int, 32>{});       // otherwise a CTA has the row
     } else if (plan.values == 8) {
-        if constexpr (BIAS || GROUPS) run(eight, integral_constant<int, 0>{});
+        if constexpr (BIAS || GROUPS || sizeof(T) == 4) run(eight, integral_constant<int, 0>{});
     } else run(sixteen, integral_constant<int, 0>{});
     return ok;
 }

@@ -38,37 +38,27 @@ __device__ __forceinline__ float logistic(float g) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
     return s;
 }
-// act(g) of a pack, and with SLOPE its derivative; the kind is the same for a whole call, so that one branch serves the pack.
-template <bool SLOPE, int V>
-__device__ __forceinline__ void gate_values(const float (&g)[V], int kind, float (&a)[V], float (&slope)[V]) {
+// g becomes act(g), and with SLOPE slope its derivative; the kind is the same for a whole call, so that one branch serves a pack.
+template <bool SLOPE, typename N, int M>
+__device__ __forceinline__ void gate_values(N (&g)[M], int kind, N (&slope)[M]) {
     if (kind == kGateLinear) {
+        if constexpr (SLOPE)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            a[i] = g[i];
-            if constexpr (SLOPE) slope[i] = 1.f;
-        }
+            for (int i = 0; i < M; ++i) slope[i] = splat<N>(1.f);
     } else if (kind == kGateSigmoid) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            a[i] = logistic(g[i]);
-            if constexpr (SLOPE) slope[i] = fmaf(-a[i], a[i], a[i]);
+        for (int i = 0; i < M; ++i) {
+            g[i] = each(g[i], logistic);
+            if constexpr (SLOPE) slope[i] = fma(mul(g[i], splat<N>(-1.f)), g[i], g[i]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float t = logistic(g[i]);
-            a[i] = g[i] * t;
-            if constexpr (SLOPE) slope[i] = fmaf(a[i], 1.f - t, t);
+        for (int i = 0; i < M; ++i) {
+            const N t = each(g[i], logistic);
+            g[i] = mul(g[i], t);
+            if constexpr (SLOPE) slope[i] = fma(g[i], fma(t, splat<N>(-1.f), splat<N>(1.f)), t);
         }
     }
-}
-template <int V>
-__device__ __forceinline__ void multiply(float (&s)[V], const float* p, int c) {
-    if (p == nullptr) return;
-    float f[V];
-    load_params(p, c, 1.f, f);
-#pragma unroll
-    for (int i = 0; i < V; ++i) s[i] *= f[i];
 }
 
 // The team's columns: K packs of V values per thread.
@@ -80,81 +70,104 @@ struct Columns {
     __device__ __forceinline__ bool has(int k) const { return at + k * step < cols; }
 };
 
-// v becomes (v - mean) * inv, inv = 1 / sqrt(mean square + eps), over the row; values outside of the row stay 0.  Returns inv.
-template <int SIZE, int V, int K>
-__device__ __forceinline__ float normalise(float (&v)[K][V], Team<SIZE>& team, const Columns<SIZE, V, K>& col, int kind, float eps, float inv_cols) {
-    if (kind == kNormNone) return 1.f;
-    if (kind == kNormLayer) {
-        float s[1] = {0.f};
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[0] += v[k][i];
-        team.sum(s);
-        const float mean = s[0] * inv_cols;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[k][i] = col.has(k) ? v[k][i] - mean : 0.f;
-    }
-    float q[1] = {0.f};
+// A thread's values of a row: K packs of V.
+template <int V, int K>
+using Values = Num<V>[K][kNums<V>];
+
+template <int V, int K>
+__device__ __forceinline__ float dot(const Values<V, K>& a, const Values<V, K>& b) {
+    Num<V> s = splat<Num<V>>(0.f);
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int i = 0; i < V; ++i) q[0] = fmaf(v[k][i], v[k][i], q[0]);
+        for (int i = 0; i < kNums<V>; ++i) s = fma(a[k][i], b[k][i], s);
+    return total(s);
+}
+template <int V, int K>
+__device__ __forceinline__ float sum_of(const Values<V, K>& a) {
+    Num<V> s = splat<Num<V>>(0.f);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < kNums<V>; ++i) s = add(s, a[k][i]);
+    return total(s);
+}
+
+// v becomes (v - mean) * inv, inv = 1 / sqrt(mean square + eps), over the row; values outside of the row are 0 and stay so.  Returns inv.
+// LAYER: the kind may be a layer norm; without it no mean is looked for.
+template <bool LAYER, int SIZE, int V, int K>
+__device__ __forceinline__ float normalise(Values<V, K>& v, Team<SIZE>& team, const Columns<SIZE, V, K>& col, int kind, float eps, float inv_cols) {
+    if (kind == kNormNone) return 1.f;
+    if constexpr (LAYER) {
+        if (kind == kNormLayer) {
+            float s[1] = {sum_of<V, K>(v)};
+            team.sum(s);
+            const Num<V> mean = splat<Num<V>>(-s[0] * inv_cols);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < kNums<V>; ++i) v[k][i] = col.has(k) ? add(v[k][i], mean) : splat<Num<V>>(0.f);
+        }
+    }
+    float q[1] = {dot<V, K>(v, v)};
     team.sum(q);
     const float inv = rsqrtf(fmaf(q[0], inv_cols, eps));
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[k][i] *= inv;
+        for (int i = 0; i < kNums<V>; ++i) v[k][i] = mul(v[k][i], splat<Num<V>>(inv));
     return inv;
 }
-
-template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-
-// The operands of a team's rows in shared memory: one or two stages, [stage][operand][k][thread].  A thread copies what it reads itself, so that
-// no barrier is needed; with two stages the next row is on its way while this one is worked on.
-template <typename T, int V, int K, int SIZE>
-struct Staged {
-    using P = Pack<T, V>;
-    P* own;
-    int stage_packs;
-    const Columns<SIZE, V, K>& col;
-    __device__ __forceinline__ Staged(uint8_t* smem, int operands, const Columns<SIZE, V, K>& c)
-        : own(reinterpret_cast<P*>(smem) + threadIdx.x), stage_packs(operands * K * static_cast<int>(blockDim.x)), col(c) {}
-    __device__ __forceinline__ P& slot(int stage, int operand, int k) const { return own[stage * stage_packs + (operand * K + k) * static_cast<int>(blockDim.x)]; }
-    __device__ __forceinline__ void copy(const void* base, int64_t ld, int64_t row, int stage, int operand) const {
-        const T* const p = static_cast<const T*>(base) + row * ld;
+// v becomes the gradient at what hat = (v - mean) * inv was formed of, given the one at hat.
+template <bool LAYER, int SIZE, int V, int K>
+__device__ __forceinline__ void through_norm(Values<V, K>& v, const Values<V, K>& hat, float inv, Team<SIZE>& team, int kind, float inv_cols) {
+    using N = Num<V>;
+    if (kind == kNormNone) return;
+    if (LAYER && kind == kNormLayer) {
+        float s[2] = {sum_of<V, K>(v), dot<V, K>(v, hat)};
+        team.sum(s);
+        const N mean = splat<N>(-s[0] * inv_cols * inv), along = splat<N>(-s[1] * inv_cols * inv);
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (!col.has(k)) continue;
-            if constexpr (sizeof(P) >= 4) copy_async<sizeof(P)>(static_cast<uint32_t>(__cvta_generic_to_shared(&slot(stage, operand, k))), p + col(k));
-            else slot(stage, operand, k).v[0] = p[col(k)];
-        }
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < kNums<V>; ++i) v[k][i] = fma(along, hat[k][i], fma(splat<N>(inv), v[k][i], mean));
+    } else {
+        float s[1] = {dot<V, K>(v, hat)};
+        team.sum(s);
+        const N along = splat<N>(-s[0] * inv_cols * inv);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < kNums<V>; ++i) v[k][i] = fma(along, hat[k][i], mul(splat<N>(inv), v[k][i]));
     }
-    __device__ __forceinline__ void get(int stage, int operand, int k, bool ok, float (&f)[V]) const { unpack(ok ? slot(stage, operand, k) : zero_pack<T, V>(), f); }
-};
-__device__ __forceinline__ void end_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// The copies of this row have landed; with two stages the next row's may be on their way.
-__device__ __forceinline__ void wait_copies(int stages) {
-    if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+template <int V>
+__device__ __forceinline__ void multiply(Num<V> (&s)[kNums<V>], const float* p, int c) {
+    if (p == nullptr) return;
+    Num<V> f[kNums<V>];
+    read_global<float, V>(p + c, f);
+#pragma unroll
+    for (int i = 0; i < kNums<V>; ++i) s[i] = mul(s[i], f[i]);
+}
+template <int V>
+__device__ __forceinline__ void add_to(Num<V> (&s)[kNums<V>], const float* p, int c) {
+    if (p == nullptr) return;
+    Num<V> f[kNums<V>];
+    read_global<float, V>(p + c, f);
+#pragma unroll
+    for (int i = 0; i < kNums<V>; ++i) s[i] = add(s[i], f[i]);
 }
 
-// A pack of the gate that a group of rows shares: it stays in the L1.
-template <typename T, int V>
-__device__ __forceinline__ void shared_gate(const T* p, float (&u)[V]) {
-    if constexpr (V == 1) {
-        u[0] = to_float(*p);
-    } else {
-        const uint4 raw = __ldg(reinterpret_cast<const uint4*>(p));
-        unpack(*reinterpret_cast<const Pack<T, V>*>(&raw), u);
-    }
+// Values as fp32 at p, or added to what is there.
+template <int V>
+__device__ __forceinline__ void write_floats(float* p, const Num<V> (&n)[kNums<V>], bool more) {
+    float f[V];
+    if constexpr (V == 1) f[0] = n[0].v;
+    else
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) unpack2(n[i].v, f[2 * i], f[2 * i + 1]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = more ? p[i] + f[i] : f[i];
 }
 
 constexpr int kNormWarpThreads = 256;            // CTA of warp teams
@@ -162,101 +175,149 @@ constexpr int kNormWarpThreads = 256;            // CTA of warp teams
 // Most threads of a CTA: a CTA team has up to 8192 / (K * V) threads.
 template <int SIZE, int V, int K>
 constexpr int kNormThreads = SIZE ? kNormWarpThreads : 8192 / (K * V);
+template <int SIZE>
+constexpr int kTeamsHere = SIZE ? kNormWarpThreads / (SIZE ? SIZE : 1) : 1;
 
-// Operands of a row that are staged: not the gate of a group, which stays for many rows.
-__host__ __device__ inline int norm_operands(const NormArgs& a) { return 1 + (a.h != nullptr) + (a.gate != nullptr && a.gate_rows == 1); }
+// What the kernels of both directions set up: scratch, barriers, the team, its columns, its pipe (teams of operands from `smem` on, zeros beyond the rows).
+#define CUTOFF_NORM_TEAM(ARGS, OPERANDS)                                                                                          \
+    extern __shared__ __align__(16) uint8_t dynamic[];                                                                           \
+    __shared__ __align__(16) float scratch[Team<SIZE>::kScratch];                                                                \
+    __shared__ __align__(8) uint64_t barriers[2 * kTeamsHere<SIZE>];                                                             \
+    Team<SIZE> team(scratch);                                                                                                    \
+    const Columns<SIZE, V, K> col(team, (ARGS).cols);                                                                            \
+    const int team_here = SIZE ? threadIdx.x / (SIZE ? SIZE : 1) : 0;                                                            \
+    const RowPipe<T, SIZE> pipe(OPERANDS, async::smem_u32(dynamic), async::smem_u32(barriers), team_here);                       \
+    if (team.rank() == 0) pipe.open();                                                                                           \
+    if constexpr (V > 1)                                                                                                         \
+        for (int s = 0; s < (OPERANDS).stages * (OPERANDS).n; ++s)                                                               \
+            _Pragma("unroll") for (int k = 0; k < K; ++k)                                                                        \
+                if (!col.has(k)) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(pipe.slots + s * (OPERANDS).slot_bytes + col(k) * static_cast<int>(sizeof(T))), "r"(0) : "memory"); \
+    async::fence_proxy_async();                                                                                                  \
+    __syncthreads();
 
-template <typename T, int V, int K, int SIZE>
-__global__ void __launch_bounds__(kNormThreads<SIZE, V, K>, 1024 / kNormThreads<SIZE, V, K>) k_residual_norm(NormArgs a, int stages) {
-    extern __shared__ __align__(16) uint8_t operands[];
-    __shared__ __align__(16) float scratch[Team<SIZE>::kScratch];
-    Team<SIZE> team(scratch);
-    const Columns<SIZE, V, K> col(team, a.cols);
-    const bool gate_rows = a.gate && a.gate_rows == 1;
-    const int at_h = 1, at_gate = at_h + (a.h != nullptr);
-    const Staged<T, V, K, SIZE> staged(operands, at_gate + gate_rows, col);
-    const int teams_here = SIZE ? blockDim.x / (SIZE ? SIZE : 1) : 1, team_here = SIZE ? threadIdx.x / (SIZE ? SIZE : 1) : 0;
-    const int teams = gridDim.x * teams_here, turns = ceil_div(a.rows, teams);        // as many for all teams of a warp: its shuffles take all lanes
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * teams_here + team_here;
-    const auto fetch = [&](int stage, int64_t row) {
-        if (row < a.rows) {
-            if (a.h) staged.copy(a.h, a.h_ld, row, stage, at_h);
-            staged.copy(a.x, a.x_ld, row, stage, 0);
-            if (gate_rows) staged.copy(a.gate, a.gate_ld, row, stage, at_gate);
-        }
-        end_copies();
-    };
-    fetch(0, first);
-    for (int turn = 0; turn < turns; ++turn) {
-        const int64_t row = first + static_cast<int64_t>(turn) * teams;
-        const int stage = stages == 2 ? turn & 1 : 0;
-        if (stages == 2) fetch(stage ^ 1, row + teams);
-        wait_copies(stages);
-        const bool mine = row < a.rows;           // a warp's last teams may have no row
-        float r[K][V];
-        if (a.h) {
+// A pack of an operand; single values beyond the row, or of a row that the team does not have, are zeros (packs beyond the row are zeros in shared memory).
+template <typename T, int V, int SIZE, int K>
+__device__ __forceinline__ void take(uint32_t row_at, const Columns<SIZE, V, K>& col, int k, bool mine, Num<V> (&f)[kNums<V>]) {
+    read_shared<T, V>(row_at + col(k) * static_cast<int>(sizeof(T)), (V > 1 || col.has(k)) && (SIZE == 0 || mine), f);
+}
+// A pack of the gate of a group of rows; zeros beyond the row (where an infinite gate would turn zeros into NaN).
+template <typename T, int V, int SIZE, int K>
+__device__ __forceinline__ void take_shared_gate(const T* row, const Columns<SIZE, V, K>& col, int k, Num<V> (&f)[kNums<V>]) {
+    read_global<T, V>(row + min(col(k), col.cols - V), f);
 #pragma unroll
-            for (int k = 0; k < K; ++k) staged.get(stage, at_h, k, mine && col.has(k), r[k]);
-            normalise(r, team, col, a.post, a.eps, a.inv_cols);
+    for (int i = 0; i < kNums<V>; ++i) f[i] = col.has(k) ? f[i] : splat<Num<V>>(0.f);
+}
+
+// Registers of a forward thread: with 16 values and their parameters 80, three CTAs of 256 threads per SM.
+template <int V, int K, bool BIAS>
+constexpr int kNormRegisters = V * K > 8 ? (BIAS ? 112 : 80) : (BIAS ? 80 : 64);
+
+// The parameters of a thread's columns stay in its registers: in the L1, beside the operands' shared memory, there is no room for them, and every row
+// would bring them from the L2 again (4096 bf16 values with gate, 16384 rows: 152 us so; 5000 rows of 2175 fp32 values 131).
+template <typename T, int V, int K, int SIZE, bool LAYER, bool BIAS>
+__global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands) {
+    using N = Num<V>;
+    constexpr int M = kNums<V>, kBias = BIAS ? K : 1;
+    CUTOFF_NORM_TEAM(a, operands)
+    const bool gate_rows = a.gate && a.gate_rows == 1;
+    const int at_h = 1, at_gate = 2;
+    const int teams = gridDim.x * kTeamsHere<SIZE>, turns = ceil_div(a.rows, teams);        // as many for all teams of a warp: its shuffles take all lanes
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kTeamsHere<SIZE> + team_here;
+    bool failed = false;                          // a wait gave up: none is made after it, and nothing is asked for
+    for (int s = 0; s < operands.stages; ++s)
+        if (first + static_cast<int64_t>(s) * teams < a.rows) pipe.fetch(s, first + static_cast<int64_t>(s) * teams, team);
+    N post_w[K][M], pre_w[K][M], post_b[kBias][M] = {}, pre_b[kBias][M] = {};       // the block's scale is part of the first and the third
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+        for (int i = 0; i < M; ++i) post_w[k][i] = pre_w[k][i] = splat<N>(col.has(k) ? 1.f : 0.f);
+        if (!col.has(k)) continue;
+        multiply<V>(post_w[k], a.post_w, col(k));
+        multiply<V>(post_w[k], a.scale, col(k));
+        multiply<V>(pre_w[k], a.pre_w, col(k));
+        if constexpr (BIAS) {
+            add_to<V>(post_b[k], a.post_b, col(k));
+            multiply<V>(post_b[k], a.scale, col(k));
+            add_to<V>(pre_b[k], a.pre_b, col(k));
+        }
+    }
+    for (int turn = 0; turn < turns; ++turn) {
+        const int64_t row = first + static_cast<int64_t>(turn) * teams, next = row + static_cast<int64_t>(operands.stages) * teams;
+        const int stage = operands.stages == 2 ? turn & 1 : 0;
+        const bool mine = row < a.rows;           // a warp's last teams may have no row
+        if (!SIZE && !mine) break;
+        failed = failed || (mine && !pipe.wait(turn));
+        const float eps = failed ? __int_as_float(0x7fc00000) : a.eps;         // what did not arrive gives NaN
+        const uint32_t x_at = pipe.template row_at<V>(stage, 0, row);
+        N r[K][M];
+        if (a.h) {
+            const uint32_t h_at = pipe.template row_at<V>(stage, at_h, row);
+#pragma unroll
+            for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, mine, r[k]);
+            normalise<LAYER, SIZE, V, K>(r, team, col, a.post, eps, a.inv_cols);
+            T* const r_row = static_cast<T*>(a.r) + row * a.r_ld;
+            const uint32_t gate_at = gate_rows ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
             const T* const group_gate =
-                static_cast<const T*>(a.gate) + (a.gate && !gate_rows ? static_cast<int64_t>(static_cast<unsigned>(row) / static_cast<unsigned>(a.gate_rows)) * a.gate_ld : 0);
+                static_cast<const T*>(a.gate) + (a.gate && !gate_rows && mine ? static_cast<int64_t>(static_cast<unsigned>(row) / static_cast<unsigned>(a.gate_rows)) * a.gate_ld : 0);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                if (!col.has(k)) continue;
-                float t[V];
-                multiply(r[k], a.post_w, col(k));
-                if (a.post_b) {
-                    load_params(a.post_b, col(k), 0.f, t);
+                N t[M], x[M];
+                take<T, V>(x_at, col, k, mine, x);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) r[k][i] += t[i];
-                }
-                multiply(r[k], a.scale, col(k));
+                for (int i = 0; i < M; ++i) r[k][i] = BIAS ? fma(r[k][i], post_w[k][i], post_b[BIAS ? k : 0][i]) : mul(r[k][i], post_w[k][i]);
                 if (a.gate) {
-                    float act[V];
-                    if (gate_rows) staged.get(stage, at_gate, k, mine, t);
-                    else if (mine) shared_gate(group_gate + col(k), t);
-                    gate_values<false>(t, a.gate_kind, act, act);
+                    if (gate_rows) take<T, V>(gate_at, col, k, mine, t);
+                    else take_shared_gate<T, V>(group_gate, col, k, t);
+                    gate_values<false>(t, a.gate_kind, t);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) r[k][i] *= act[i];
+                    for (int i = 0; i < M; ++i) r[k][i] = fma(r[k][i], t[i], x[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < M; ++i) r[k][i] = add(r[k][i], x[i]);
                 }
-                staged.get(stage, 0, k, mine, t);
-#pragma unroll
-                for (int i = 0; i < V; ++i) r[k][i] = mine ? r[k][i] + t[i] : 0.f;
-                if (a.r && mine) store_pack<T, V>(static_cast<T*>(a.r) + row * a.r_ld + col(k), r[k]);
+                if (a.r) write_global<T, V>(r_row + col(k), mine && col.has(k), r[k]);
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < K; ++k) staged.get(stage, 0, k, mine && col.has(k), r[k]);
+            for (int k = 0; k < K; ++k) take<T, V>(x_at, col, k, mine, r[k]);
         }
-        if (stages == 1) fetch(0, row + teams);   // this row's values have been used
+        // this row's values have been used, by all of the team
+        if (turn + operands.stages < turns) {
+            team.sync();
+            if (!failed && next < a.rows) pipe.fetch(stage, next, team);
+        }
         if (!a.n) continue;
-        normalise(r, team, col, a.pre, a.eps, a.inv_cols);
-        uint32_t top = 0;
+        normalise<LAYER, SIZE, V, K>(r, team, col, a.pre, eps, a.inv_cols);
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (!col.has(k)) continue;
-            multiply(r[k], a.pre_w, col(k));
-            if (a.pre_b) {
-                float b[V];
-                load_params(a.pre_b, col(k), 0.f, b);
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int i = 0; i < V; ++i) r[k][i] += b[i];
-            }
-            if (!a.n_scale) {
-                if (mine) store_pack<T, V>(static_cast<T*>(a.n) + row * a.n_ld + col(k), r[k]);
-            } else {
+            for (int i = 0; i < M; ++i) r[k][i] = BIAS ? fma(r[k][i], pre_w[k][i], pre_b[BIAS ? k : 0][i]) : mul(r[k][i], pre_w[k][i]);
+        if (!a.n_scale) {
+            T* const n_row = static_cast<T*>(a.n) + row * a.n_ld;
 #pragma unroll
-                for (int i = 0; i < V; ++i) top = max(top, magnitude_bits(r[k][i]));
-            }
+            for (int k = 0; k < K; ++k) write_global<T, V>(n_row + col(k), mine && col.has(k), r[k]);
+            continue;
         }
-        if (!a.n_scale) continue;
+        uint32_t top = 0;                         // beyond the row everything is zero, the parameters too
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < M; ++i) each(r[k][i], [&](float v) { top = max(top, magnitude_bits(v)); return v; });
         const RowScale q = row_scale(team.top(top));
         if (!mine) continue;
         if (team.rank() == 0) a.n_scale[row] = q.scale;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (col.has(k)) store_quantised<V>(static_cast<int8_t*>(a.n) + row * a.n_ld + col(k), r[k], q.inverse);
+        for (int k = 0; k < K; ++k) {
+            if (!col.has(k)) continue;
+            float f[V];
+            if constexpr (V == 1) f[0] = r[k][0].v;
+            else
+#pragma unroll
+                for (int i = 0; i < M; ++i) unpack2(r[k][i].v, f[2 * i], f[2 * i + 1]);
+            store_quantised<V>(static_cast<int8_t*>(a.n) + row * a.n_ld + col(k), f, q.inverse);
+        }
     }
+    if (failed) pipe.drain();
 }
 
 // ---- backward ----------------------------------------------------------------------------------------------------------
@@ -269,213 +330,197 @@ struct NormGradArgs {
     float* sums;                                  // [CTAs][2 or 4][cols]: sum e * hat, sum d_n * r_hat, with BIAS also sum e, sum d_n
     float* gate_sums;                             // [teams][2][cols]: of the team's first and last group, where another team has the rest
     int teams;
-    int stages;                                   // rows of a team in shared memory: 2, the next one on its way, or 1
+    int param_bytes;                              // offset in shared memory of the parameters: scale * post_w, pre_w, with BIAS scale * post_b
 };
 // Rows of team t.
-__device__ __forceinline__ int first_row_of(int t, int teams, int rows) { return static_cast<int>(static_cast<int64_t>(rows) * t / teams); }
-
-// Operands that a row of the backward pass reads; with GROUPS the gate is not among them, it stays for many rows and is read through the L1.
-template <bool GROUPS>
-__host__ __device__ inline int grad_operands(const NormGradArgs& g) { return 1 + (g.f.h != nullptr) + (!GROUPS && g.f.gate) + (g.d_r != nullptr) + (g.d_n != nullptr); }
+__device__ __forceinline__ int first_row_of(int t, int teams, int rows) { return rows / teams * t + min(t, rows % teams); }
 
 constexpr int kGradThreads = 512;                 // most threads of a CTA: 128 registers each
 
 // GROUPS: a gate for each group of rows, whose gradient is a sum over them.  BIAS: either norm has one, so that the plain sums are needed.
-// The operands of a team's next row are on their way to shared memory while this one is worked on; every thread copies what it reads itself, so that no barrier
-// is needed for them.
-template <typename T, int V, int K, int SIZE, bool BIAS, bool GROUPS>
-__global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ? 2 : 1) k_residual_norm_grad(NormGradArgs g) {
-    extern __shared__ __align__(16) uint8_t operands[];       // [stage][operand][k][thread]; afterwards [cols] sums
-    __shared__ __align__(16) float scratch[Team<SIZE>::kScratch];
+// SHARED: the parameters are in shared memory (there is no room for them beside one row of five fp32 operands of 8192 values).
+template <typename T, int V, int K, int SIZE, bool BIAS, bool GROUPS, bool LAYER, bool SHARED>
+__global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ? 2 : 1) k_residual_norm_grad(NormGradArgs g, const __grid_constant__ RowOperands operands) {
+    using N = Num<V>;
+    constexpr int M = kNums<V>;
     const NormArgs& a = g.f;
-    Team<SIZE> team(scratch);
-    const Columns<SIZE, V, K> col(team, a.cols);
-    const int teams_here = SIZE ? blockDim.x / (SIZE ? SIZE : 1) : 1, team_here = SIZE ? threadIdx.x / (SIZE ? SIZE : 1) : 0;
-    const int t = blockIdx.x * teams_here + team_here;
+    CUTOFF_NORM_TEAM(a, operands)
+    const int t = blockIdx.x * kTeamsHere<SIZE> + team_here;
     const int first = first_row_of(t, g.teams, a.rows), last = first_row_of(t + 1, g.teams, a.rows);
     const int turns = ceil_div(a.rows, g.teams);               // the same for all teams of a warp: its shuffles take all lanes
     constexpr int kBias = BIAS ? K : 1, kGroups = GROUPS ? K : 1;
-    float e_hat[K][V] = {}, n_hat[K][V] = {}, e_sum[kBias][V] = {}, n_sum[kBias][V] = {}, gate_sum[kGroups][V] = {};
+    N e_hat[K][M] = {}, n_hat[K][M] = {}, e_sum[kBias][M] = {}, n_sum[kBias][M] = {}, gate_sum[kGroups][M] = {};
 
     // places of the operands in a stage
     const bool has_gate_rows = !GROUPS && a.gate != nullptr;
-    const int at_h = 1, at_gate = at_h + (a.h != nullptr), at_r = at_gate + has_gate_rows, at_n = at_r + (g.d_r != nullptr), n_operands = at_n + (g.d_n != nullptr);
-    const Staged<T, V, K, SIZE> staged(operands, n_operands, col);
-    const auto fetch = [&](int stage, int row) {
-        if (row < last) {
-            if (a.h) staged.copy(a.h, a.h_ld, row, stage, at_h);
-            staged.copy(a.x, a.x_ld, row, stage, 0);
-            if (has_gate_rows) staged.copy(a.gate, a.gate_ld, row, stage, at_gate);
-            if (g.d_n) staged.copy(g.d_n, g.d_n_ld, row, stage, at_n);
-            if (g.d_r) staged.copy(g.d_r, g.d_r_ld, row, stage, at_r);
-        }
-        end_copies();
-    };
-    const auto get = [&](int stage, int operand, int k, bool ok, float (&f)[V]) { staged.get(stage, operand, k, ok, f); };
-
+    const int at_h = 1, at_gate = at_h + (a.h != nullptr), at_r = at_gate + has_gate_rows, at_n = at_r + (g.d_r != nullptr);
     dependency_wait();
-    fetch(0, first);
+    bool failed = false;                          // a wait gave up: none is made after it, and nothing is asked for
+    for (int s = 0; s < operands.stages; ++s)
+        if (first + s < last) pipe.fetch(s, first + s, team);
+    // the parameters: in the L1, beside the operands, there is no room for them
+    const uint32_t params = async::smem_u32(dynamic) + g.param_bytes;
+    const int param_cols = team.size() * V * K;               // zeros beyond the row
+    const auto param_of = [&](int which, int k, N (&f)[M]) {
+        if constexpr (SHARED) {
+            read_shared_params<V>(params + 4 * (which * param_cols + col(k)), f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < M; ++i) f[i] = splat<N>(!col.has(k) || (which == 2 && !a.post_b) ? 0.f : 1.f);
+            if (!col.has(k)) return;
+            multiply<V>(f, which == 0 ? a.post_w : which == 1 ? a.pre_w : a.post_b, col(k));
+            if (which != 1) multiply<V>(f, a.scale, col(k));
+        }
+    };
+    if constexpr (SHARED) {
+        float* const p = reinterpret_cast<float*>(dynamic + g.param_bytes);
+        for (int c = threadIdx.x; c < param_cols; c += blockDim.x) {
+            const bool in = c < a.cols;
+            const float s = in ? a.scale ? a.scale[c] : 1.f : 0.f;
+            p[c] = in && a.post_w ? s * a.post_w[c] : s;
+            p[param_cols + c] = in ? a.pre_w ? a.pre_w[c] : 1.f : 0.f;
+            if constexpr (BIAS) p[2 * param_cols + c] = in && a.post_b ? s * a.post_b[c] : 0.f;
+        }
+    }
+    __syncthreads();
     for (int turn = 0; turn < turns; ++turn) {
-        const int row = first + turn, stage = g.stages == 2 ? turn & 1 : 0;
+        const int row = first + turn, stage = operands.stages == 2 ? turn & 1 : 0;
         const bool mine = row < last;
-        if (g.stages == 2) fetch(stage ^ 1, row + 1);
-        wait_copies(g.stages);
+        if (!SIZE && !mine) break;
+        failed = failed || (mine && !pipe.wait(turn));
+        const float eps = failed ? __int_as_float(0x7fc00000) : a.eps;         // what did not arrive gives NaN
         const int group = GROUPS && mine ? row / a.gate_rows : 0;
         const T* const group_gate = static_cast<const T*>(a.gate) + group * a.gate_ld;
-        const auto gate_of = [&](int k, float (&u)[V]) {
-            if constexpr (GROUPS) {
-                shared_gate(group_gate + col(k), u);
-            } else {
-                get(stage, at_gate, k, mine, u);
-            }
+        const uint32_t gate_at = has_gate_rows ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
+        const auto gate_of = [&](int k, N (&u)[M]) {
+            if constexpr (GROUPS) take_shared_gate<T, V>(group_gate, col, k, u);
+            else take<T, V>(gate_at, col, k, mine, u);
         };
-        float hat[K][V], r[K][V], d[K][V];        // d: the whole gradient at r
+        N hat[K][M], d[K][M];                     // d: the whole gradient at r
         float h_inv = 1.f;
         if (a.h) {
+            const uint32_t h_at = pipe.template row_at<V>(stage, at_h, row);
 #pragma unroll
-            for (int k = 0; k < K; ++k) get(stage, at_h, k, mine && col.has(k), hat[k]);
-            h_inv = normalise(hat, team, col, a.post, a.eps, a.inv_cols);
+            for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, mine, hat[k]);
+            h_inv = normalise<LAYER, SIZE, V, K>(hat, team, col, a.post, eps, a.inv_cols);
         }
+        const uint32_t d_r_at = g.d_r ? pipe.template row_at<V>(stage, at_r, row) : 0u;
         if (g.d_n) {
+            N r[K][M];
+            const uint32_t x_at = pipe.template row_at<V>(stage, 0, row), d_n_at = pipe.template row_at<V>(stage, at_n, row);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                if (a.h && col.has(k)) {
-                    float u[V], act[V];
+                take<T, V>(x_at, col, k, mine, r[k]);
+                if (!a.h) continue;
+                N w[M], u[M];
+                param_of(0, k, w);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) r[k][i] = hat[k][i];
-                    multiply(r[k], a.post_w, col(k));
-                    if constexpr (BIAS) {
-                        load_params(a.post_b, col(k), 0.f, u);
+                for (int i = 0; i < M; ++i) w[i] = mul(w[i], hat[k][i]);
+                if constexpr (BIAS) {
+                    param_of(2, k, u);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) r[k][i] += u[i];
-                    }
-                    multiply(r[k], a.scale, col(k));
-                    if (a.gate) {
-                        gate_of(k, u);
-                        gate_values<false>(u, a.gate_kind, act, act);
+                    for (int i = 0; i < M; ++i) w[i] = add(w[i], u[i]);
+                }
+                if (a.gate) {
+                    gate_of(k, u);
+                    gate_values<false>(u, a.gate_kind, u);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) r[k][i] *= act[i];
-                    }
+                    for (int i = 0; i < M; ++i) r[k][i] = fma(w[i], u[i], r[k][i]);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) r[k][i] = 0.f;
-                }
-                float x[V];
-                get(stage, 0, k, mine && col.has(k), x);
-#pragma unroll
-                for (int i = 0; i < V; ++i) r[k][i] += x[i];
-            }
-            const float r_inv = normalise(r, team, col, a.pre, a.eps, a.inv_cols);
-            float s[2] = {0.f, 0.f};              // sums of the gradient at r_hat, and of its products with r_hat
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float dn[V];
-                get(stage, at_n, k, mine && col.has(k), dn);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    n_hat[k][i] = fmaf(dn[i], r[k][i], n_hat[k][i]);
-                    if constexpr (BIAS) n_sum[k][i] += dn[i];
-                }
-                if (col.has(k)) multiply(dn, a.pre_w, col(k));
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    d[k][i] = dn[i];
-                    s[0] += dn[i];
-                    s[1] = fmaf(dn[i], r[k][i], s[1]);
+                    for (int i = 0; i < M; ++i) r[k][i] = add(r[k][i], w[i]);
                 }
             }
-            if (a.pre != kNormNone) {
-                team.sum(s);
-                const float mean = a.pre == kNormLayer ? s[0] * a.inv_cols : 0.f, along = s[1] * a.inv_cols;
+            if (SIZE != 0 && !mine)               // a bias would be left of a row that there is not
 #pragma unroll
                 for (int k = 0; k < K; ++k)
 #pragma unroll
-                    for (int i = 0; i < V; ++i) d[k][i] = r_inv * (fmaf(-along, r[k][i], d[k][i]) - mean);
+                    for (int i = 0; i < M; ++i) r[k][i] = splat<N>(0.f);
+            const float r_inv = normalise<LAYER, SIZE, V, K>(r, team, col, a.pre, eps, a.inv_cols);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                take<T, V>(d_n_at, col, k, mine, d[k]);
+#pragma unroll
+                for (int i = 0; i < M; ++i) {
+                    n_hat[k][i] = fma(d[k][i], r[k][i], n_hat[k][i]);
+                    if constexpr (BIAS) n_sum[k][i] = add(n_sum[k][i], d[k][i]);
+                }
+                N w[M];
+                param_of(1, k, w);
+#pragma unroll
+                for (int i = 0; i < M; ++i) d[k][i] = mul(d[k][i], w[i]);
+            }
+            through_norm<LAYER, SIZE, V, K>(d, r, r_inv, team, a.pre, a.inv_cols);
+            if (g.d_r) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    N dr[M];
+                    take<T, V>(d_r_at, col, k, mine, dr);
+#pragma unroll
+                    for (int i = 0; i < M; ++i) d[k][i] = add(d[k][i], dr[i]);
+                }
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) d[k][i] = 0.f;
+            for (int k = 0; k < K; ++k) take<T, V>(d_r_at, col, k, mine, d[k]);
         }
-        if (g.d_r) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float dr[V];
-                get(stage, at_r, k, mine && col.has(k), dr);
-#pragma unroll
-                for (int i = 0; i < V; ++i) d[k][i] += dr[i];
-            }
-        }
-        if (g.d_x && mine) {
+        if (g.d_x) {
             T* const out = static_cast<T*>(g.d_x) + row * g.d_x_ld;
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (col.has(k)) store_pack<T, V>(out + col(k), d[k]);
+            for (int k = 0; k < K; ++k) write_global<T, V>(out + col(k), mine && col.has(k), d[k]);
         }
         if (a.h) {
-            float s[2] = {0.f, 0.f};              // the same two sums at hat
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                if (!col.has(k)) continue;
-                float w[V], scale[V], at_gate_value[V];
-                load_params(a.post_w, col(k), 1.f, w);
-                load_params(a.scale, col(k), 1.f, scale);
-                if (a.gate && (GROUPS || g.d_gate)) {
-                    float p[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) p[i] = hat[k][i] * w[i];
-                    if constexpr (BIAS) {
-                        float b[V];
-                        load_params(a.post_b, col(k), 0.f, b);
-#pragma unroll
-                        for (int i = 0; i < V; ++i) p[i] += b[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < V; ++i) at_gate_value[i] = d[k][i] * scale[i] * p[i];
-                }
+                N w[M];                           // scale * post_w; beyond the row it is zero, whatever a layer norm's gradient left in d
+                param_of(0, k, w);
                 if (a.gate) {
-                    float u[V], act[V], slope[V];
+                    N u[M], slope[M];
                     gate_of(k, u);
-                    if constexpr (GROUPS) {
-                        gate_values<false>(u, a.gate_kind, act, slope);
+                    if (GROUPS || g.d_gate) {
+                        gate_values<!GROUPS>(u, a.gate_kind, slope);
+                        N p[M];
 #pragma unroll
-                        for (int i = 0; i < V; ++i) gate_sum[k][i] += at_gate_value[i];
-                    } else if (g.d_gate) {
-                        gate_values<true>(u, a.gate_kind, act, slope);
+                        for (int i = 0; i < M; ++i) p[i] = mul(hat[k][i], w[i]);
+                        if constexpr (BIAS) {
+                            N b[M];
+                            param_of(2, k, b);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) slope[i] *= at_gate_value[i];
-                        if (mine) store_pack<T, V>(static_cast<T*>(g.d_gate) + row * g.d_gate_ld + col(k), slope);
+                            for (int i = 0; i < M; ++i) p[i] = add(p[i], b[i]);
+                        }
+                        if constexpr (GROUPS) {
+#pragma unroll
+                            for (int i = 0; i < M; ++i) gate_sum[k][i] = fma(d[k][i], p[i], gate_sum[k][i]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], mul(d[k][i], p[i]));
+                            write_global<T, V>(static_cast<T*>(g.d_gate) + row * g.d_gate_ld + col(k), mine && col.has(k), slope);
+                        }
                     } else {
-                        gate_values<false>(u, a.gate_kind, act, slope);
+                        gate_values<false>(u, a.gate_kind, slope);
                     }
 #pragma unroll
-                    for (int i = 0; i < V; ++i) d[k][i] *= act[i];
+                    for (int i = 0; i < M; ++i) d[k][i] = mul(d[k][i], u[i]);
                 }
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    e_hat[k][i] = fmaf(d[k][i], hat[k][i], e_hat[k][i]);
-                    if constexpr (BIAS) e_sum[k][i] += d[k][i];
-                    d[k][i] *= scale[i] * w[i];
-                    s[0] += d[k][i];
-                    s[1] = fmaf(d[k][i], hat[k][i], s[1]);
+                for (int i = 0; i < M; ++i) {
+                    e_hat[k][i] = fma(d[k][i], hat[k][i], e_hat[k][i]);
+                    if constexpr (BIAS) e_sum[k][i] = add(e_sum[k][i], d[k][i]);
+                    d[k][i] = mul(d[k][i], w[i]);
                 }
             }
+        }
+        // this row's values have been used, by all of the team
+        if (turn + operands.stages < turns) {
+            team.sync();
+            if (!failed && row + operands.stages < last) pipe.fetch(stage, row + operands.stages, team);
+        }
+        if (a.h) {
             if (g.d_h) {
-                if (a.post != kNormNone) {
-                    team.sum(s);
-                    const float mean = a.post == kNormLayer ? s[0] * a.inv_cols : 0.f, along = s[1] * a.inv_cols;
+                through_norm<LAYER, SIZE, V, K>(d, hat, h_inv, team, a.post, a.inv_cols);
+                T* const out = static_cast<T*>(g.d_h) + row * g.d_h_ld;
 #pragma unroll
-                    for (int k = 0; k < K; ++k)
-#pragma unroll
-                        for (int i = 0; i < V; ++i) d[k][i] = h_inv * (fmaf(-along, hat[k][i], d[k][i]) - mean);
-                }
-                if (mine) {
-                    T* const out = static_cast<T*>(g.d_h) + row * g.d_h_ld;
-#pragma unroll
-                    for (int k = 0; k < K; ++k)
-                        if (col.has(k)) store_pack<T, V>(out + col(k), d[k]);
-                }
+                for (int k = 0; k < K; ++k) write_global<T, V>(out + col(k), mine && col.has(k), d[k]);
             }
             if constexpr (GROUPS) {
                 // the last row of a group, or of this team: the sum is the gradient, or this team's part of it
@@ -487,45 +532,39 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                     for (int k = 0; k < K; ++k) {
                         if (col.has(k)) {
                             if (whole) {
-                                float u[V], act[V], slope[V];
+                                N u[M], slope[M];
                                 gate_of(k, u);
-                                gate_values<true>(u, a.gate_kind, act, slope);
+                                gate_values<true>(u, a.gate_kind, slope);
 #pragma unroll
-                                for (int i = 0; i < V; ++i) slope[i] *= gate_sum[k][i];
-                                if (g.d_gate) store_pack<T, V>(static_cast<T*>(g.d_gate) + group * g.d_gate_ld + col(k), slope);
+                                for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], gate_sum[k][i]);
+                                if (g.d_gate) write_global<T, V>(static_cast<T*>(g.d_gate) + group * g.d_gate_ld + col(k), true, slope);
                             } else {
-#pragma unroll
-                                for (int i = 0; i < V; ++i) part[col(k) + i] = gate_sum[k][i];
+                                write_floats<V>(part + col(k), gate_sum[k], false);
                             }
                         }
 #pragma unroll
-                        for (int i = 0; i < V; ++i) gate_sum[k][i] = 0.f;
+                        for (int i = 0; i < M; ++i) gate_sum[k][i] = splat<N>(0.f);
                     }
                 }
             }
         }
-        if (g.stages == 1) fetch(0, row + 1);     // this row's values have been used
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (failed) pipe.drain();
     // this CTA's sums
     float* const out = g.sums + static_cast<int64_t>(blockIdx.x) * (BIAS ? 4 : 2) * a.cols;
-    float* const column_sums = reinterpret_cast<float*>(operands);
+    float* const column_sums = reinterpret_cast<float*>(dynamic);
     if constexpr (SIZE != 0) __syncthreads();     // nobody reads operands any more
-    const auto put = [&](float* to, const float (&v)[K][V]) {
+    const auto put = [&](float* to, const N (&v)[K][M]) {
         if constexpr (SIZE == 0) {
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (col.has(k))
-#pragma unroll
-                    for (int i = 0; i < V; ++i) to[col(k) + i] = v[k][i];
+                if (col.has(k)) write_floats<V>(to + col(k), v[k], false);
         } else {
-            for (int w = 0; w < teams_here; ++w) {
+            for (int w = 0; w < kTeamsHere<SIZE>; ++w) {
                 if (w == team_here)
 #pragma unroll
                     for (int k = 0; k < K; ++k)
-                        if (col.has(k))
-#pragma unroll
-                            for (int i = 0; i < V; ++i) column_sums[col(k) + i] = w ? column_sums[col(k) + i] + v[k][i] : v[k][i];
+                        if (col.has(k)) write_floats<V>(column_sums + col(k), v[k], w > 0);
                 __syncthreads();
             }
             for (int c = threadIdx.x; c < a.cols; c += blockDim.x) to[c] = column_sums[c];
@@ -546,9 +585,9 @@ struct NormFinishArgs {
     int column_blocks;                            // the grid's first blocks: the parameters; the others: the groups' gates
     float *d_scale, *d_post_w, *d_post_b, *d_pre_w, *d_pre_b;      // each may be null
 };
-constexpr int kFinishColumns = 32, kFinishSlices = 16;
+constexpr int kFinishColumns = 8, kFinishSlices = 64;          // eight columns are a sector
 
-// The parameters' gradients from the CTAs' sums (32 columns per block, the CTAs in 16 interleaved parts), and the gradients of gates whose rows
+// The parameters' gradients from the CTAs' sums (8 columns per block, the CTAs in 64 interleaved parts), and the gradients of gates whose rows
 // several teams had.
 template <typename T>
 __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_finish(NormFinishArgs q) {
@@ -562,18 +601,15 @@ __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_fi
             if (first == last) continue;
             const int64_t group = (last - 1) / a.gate_rows, start = group * a.gate_rows, end = min(start + a.gate_rows, static_cast<int64_t>(a.rows));
             if (start < first || end <= last) continue;
+            int stop = t + 1;                     // the first team that begins behind the group; teams without rows are all at the end
+            while (stop < q.g.teams && first_row_of(stop, q.g.teams, a.rows) < end) ++stop;
             for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
                 float s = q.g.gate_sums[(2 * static_cast<int64_t>(t) + 1) * a.cols + c];
-                int at = last;
-                for (int v = t + 1; at < end; ++v) {
-                    const int next = first_row_of(v + 1, q.g.teams, a.rows);
-                    if (next > at) s += q.g.gate_sums[2 * static_cast<int64_t>(v) * a.cols + c];
-                    at = next;
-                }
-                const float u[1] = {to_float(static_cast<const T*>(a.gate)[group * a.gate_ld + c])};
-                float act[1], slope[1];
-                gate_values<true>(u, a.gate_kind, act, slope);
-                from_float(static_cast<T*>(q.g.d_gate)[group * q.g.d_gate_ld + c], s * slope[0]);
+#pragma unroll 8                                   // loads that wait for nothing
+                for (int v = t + 1; v < stop; ++v) s += q.g.gate_sums[2 * static_cast<int64_t>(v) * a.cols + c];
+                F1 u[1] = {F1{to_float(static_cast<const T*>(a.gate)[group * a.gate_ld + c])}}, slope[1];
+                gate_values<true>(u, a.gate_kind, slope);
+                from_float(static_cast<T*>(q.g.d_gate)[group * q.g.d_gate_ld + c], s * slope[0].v);
             }
         }
         return;
@@ -594,7 +630,6 @@ __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_fi
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         s[i] = 0.f;
-#pragma unroll
         for (int j = 0; j < kFinishSlices; ++j) s[i] += part[i][j][x];
     }
     const float w = a.post_w ? a.post_w[c] : 1.f, b = a.post_b ? a.post_b[c] : 0.f, scale = a.scale ? a.scale[c] : 1.f;
@@ -612,10 +647,10 @@ struct GradPlan {
     int lanes, values, threads, per_sm, ctas, teams;
 };
 constexpr int kMostSms = 160, kMostTeamRows = 1024;          // a team adds at most this many rows in a row
-inline GradPlan grad_plan(int rows, int cols, bool many_sums, int sms) {
+inline GradPlan grad_plan(int rows, int cols, int type_size, bool many_sums, int sms) {
     GradPlan p;
     p.lanes = cols <= 32 ? 4 : cols <= 128 ? 16 : cols <= 256 || (cols <= 512 && !many_sums) ? 32 : 0;
-    p.values = p.lanes ? (cols <= 256 ? 8 : 16) : many_sums && cols <= 8 * kGradThreads ? 8 : 16;
+    p.values = p.lanes ? (cols <= 256 ? 8 : 16) : (many_sums || type_size == 4) && cols <= 8 * kGradThreads ? 8 : 16;
     p.threads = p.lanes ? kNormWarpThreads : ceil_div(ceil_div(cols, p.values), 32) * 32;
     p.per_sm = kGradThreads / p.threads;                      // by the registers; shared memory may allow fewer
     const int per_cta = p.lanes ? p.threads / p.lanes : 1;
