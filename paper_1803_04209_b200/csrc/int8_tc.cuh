@@ -8,6 +8,11 @@
 // counts is that all SMs stream: the K blocks of a tile are split over the CTAs of a cluster, which exchange their partial sums through
 // distributed shared memory (integers: in any order the same), each finishing its share of the tokens.
 //
+// k_product_pair: for many tokens and outputs.  A cluster of two CTAs works on tiles of 256 channels x 256 tokens with instructions that span both SMs
+// (cta_group::2): each CTA brings in its own 128 channels and half of the tokens, 32 KB for each 128 values of k instead of 48, and keeps the
+// sums of its own channels, twice 256 columns of tensor memory, so that one tile's epilogue runs under the next tile's products.
+// Persistent; tiles are taken in blocks of kPairGroup rows of tiles, so that what runs at a time shares operands in the L2.
+//
 // Every wait on an mbarrier is bounded as in the emission kernels.  The call has no status to write to: a tile whose wait gave up is NaN.
 #pragma once
 #include "int8_product.cuh"
@@ -208,6 +213,216 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
     if (warp == 1) {
         tc::tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Tile::kColumns) : "memory");
+    }
+}
+
+// ---- pairs of SMs ------------------------------------------------------------------------------------------------------
+constexpr int kPairTokens = 256;                  // tokens per tile; each CTA brings in half of them
+constexpr int kPairStageBytes = kProdABytes + kPairTokens / 2 * kProdK;
+constexpr int kPairStages = 6;
+constexpr int kPairEpiWarps = 8;
+constexpr int kPairThreads = (2 + kPairEpiWarps) * 32;
+constexpr int kPairGroup = 8;
+constexpr int kPairTail = 256 + kPairEpiWarps * 128 * 4;                    // barriers, flags; the tokens' scales of each epilogue warp
+constexpr size_t kPairSmem = 1024 + kPairStages * kPairStageBytes + kPairTail;
+
+__device__ __forceinline__ void umma_s8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// Tile t of the order: blocks of kPairGroup channel tiles, within a block token tile by token tile.
+struct PairTile {
+    int channels, tokens;
+};
+__device__ __forceinline__ PairTile pair_tile(int t, int channel_tiles, int token_tiles) {
+    const int block = t / (kPairGroup * token_tiles), first = block * kPairGroup, rows = min(kPairGroup, channel_tiles - first);
+    const int in = t - first * token_tiles;
+    return PairTile{first + in % rows, in / rows};
+}
+
+template <typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+k_product_pair(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, ProductArgs p, int channel_tiles, int token_tiles) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u;
+    uint8_t* const tail = smem_raw + (ring - raw) + kPairStages * kPairStageBytes;
+    const uint32_t bars = smem_u32(tail);
+    const auto full = [&](int s) { return bars + 8 * s; };                              // the leader's is the one used
+    const auto empty = [&](int s) { return bars + 8 * (kPairStages + s); };
+    const auto acc_full = [&](int b) { return bars + 8 * (2 * kPairStages + b); };
+    const auto acc_empty = [&](int b) { return bars + 8 * (2 * kPairStages + 2 + b); };
+    const auto peer_free = [&](int b) { return bars + 8 * (2 * kPairStages + 4 + b); }; // the leader's: the peer's epilogue has emptied accumulator b
+    const uint32_t drain = bars + 8 * (2 * kPairStages + 6);
+    volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + 8 * (2 * kPairStages + 7));
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(tail + 8 * (2 * kPairStages + 7) + 8);
+    static_assert(8 * (2 * kPairStages + 7) + 16 <= 256, "barriers, tensor-memory address and abort flag");
+    float* const scales = reinterpret_cast<float*>(tail + 256);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = tc::cluster_ctarank();
+    const int cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1, total = channel_tiles * token_tiles, blocks = ceil_div(p.k, kProdK);
+    DevState* const none = nullptr;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kPairStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full(b), 1);
+            mbar_init(acc_empty(b), kPairEpiWarps);
+            mbar_init(peer_free(b), 1);
+        }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::cluster_sync_all();               // the peer's barriers and tensor memory exist before anything reaches across
+    tc::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    dependency_wait();
+
+    if (warp == 0) {
+        // both CTAs: their own 128 channels, their half of the tokens
+        int s = 0;
+        uint32_t phase = 0;
+        const uint32_t leader_full = tc::map_to_cta(bars, 0u);
+        bool ok = true;
+        for (int t = cluster; ok && t < total; t += clusters) {
+            const PairTile tile = pair_tile(t, channel_tiles, token_tiles);
+            const int n0 = tile.channels * 2 * kProdM + static_cast<int>(rank) * kProdM, m0 = tile.tokens * kPairTokens + static_cast<int>(rank) * (kPairTokens / 2);
+            for (int kb = 0; kb < blocks; ++kb) {
+                ok = mbar_wait(empty(s), phase ^ 1u, abort_flag, none);
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t dst = ring + s * kPairStageBytes, bar = leader_full + 8 * s;
+                    // The leader expects the bytes of both CTAs; the peer's copies are counted there, if need be before they are expected.  (An
+                    // arrival from the peer, a release across the cluster, takes its producer 0.8 us for each stage: 8192 x 8192 x 8192 718 us.)
+                    if (rank == 0) mbar_arrive_expect_tx(full(s), 2 * kPairStageBytes);
+                    tc::tma_load_2d_pair(dst, &map_b, kb * kProdK, n0, bar);
+                    tc::tma_load_2d_pair(dst + kProdABytes, &map_a, kb * kProdK, m0, bar);
+                }
+                __syncwarp();
+                if (++s == kPairStages) { s = 0; phase ^= 1u; }
+            }
+        }
+        if (!ok) {
+            // the copies still in flight land within microseconds; they get a bounded while
+            const unsigned long long t0 = global_ns();
+            while (global_ns() - t0 < 200000ull) {}
+        }
+    } else if (warp == 1 && rank != 0) {
+        // the peer: tells the leader when its epilogue has emptied an accumulator
+        int acc = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        const uint32_t leader = tc::map_to_cta(peer_free(0), 0u);
+        for (int t = cluster; ok && t < total; t += clusters) {
+            ok = mbar_wait(acc_empty(acc), phase, abort_flag, none);
+            if (!ok) break;
+            if (lane == 0) mbar_arrive_cluster(leader + 8 * acc);
+            __syncwarp();
+            if (++acc == 2) { acc = 0; phase ^= 1u; }
+        }
+    } else if (warp == 1) {
+        // the leader: issues the products of the pair
+        int s = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        bool ok = true;
+        for (int t = cluster; ok && t < total; t += clusters) {
+            ok = mbar_wait(acc_empty(acc), acc_phase ^ 1u, abort_flag, none) && mbar_wait(peer_free(acc), acc_phase ^ 1u, abort_flag, none);
+            if (!ok) break;
+            tc::tc_fence_after();
+            const uint32_t d = tmem + acc * kPairTokens;
+            for (int kb = 0; kb < blocks; ++kb) {
+                ok = mbar_wait(full(s), phase, abort_flag, none);
+                if (!ok) break;
+                tc::tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t at = ring + s * kPairStageBytes;
+                    const uint64_t a_desc = tc::make_smem_desc(at), b_desc = tc::make_smem_desc(at + kProdABytes);
+#pragma unroll
+                    for (int k = 0; k < kProdK / 32; ++k) umma_s8_pair(d, a_desc + 2 * k, b_desc + 2 * k, instr_desc_s8(kPairTokens, 2 * kProdM), kb | k);
+                    tc::umma_commit_pair(empty(s));
+                    if (kb == blocks - 1) tc::umma_commit_pair(acc_full(acc));
+                }
+                __syncwarp();
+                if (++s == kPairStages) { s = 0; phase ^= 1u; }
+            }
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+        if (!ok) {
+            if (elect_one()) tc::umma_commit_pair(drain, 1);
+            __syncwarp();
+            mbar_wait_quiet(drain, 0u);
+        }
+        __syncwarp();
+    } else {
+        // both CTAs: a warp has 32 channels x 128 tokens
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        float* const scale = scales + (warp - 2) * 128;
+        int acc = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int t = cluster; t < total; t += clusters) {
+            const PairTile tile = pair_tile(t, channel_tiles, token_tiles);
+            const int channel = tile.channels * 2 * kProdM + static_cast<int>(rank) * kProdM + quarter * 32 + lane;
+            const int64_t m0 = static_cast<int64_t>(tile.tokens) * kPairTokens + half * 128;
+            const int here = static_cast<int>(p.m - m0 < 128 ? p.m - m0 : 128);          // tokens of this warp, none if it is <= 0
+            const bool has = channel < p.n;
+            __syncwarp();
+            for (int i = lane; i < here; i += 32) scale[i] = p.a_scale[m0 + i];
+            __syncwarp();
+            const float b_scale = has ? p.b_scale[channel] : 0.f, bias = has && p.bias ? p.bias[channel] : 0.f;
+            // after a wait that gave up the tiles that are left are marked, without another wait
+            ok = ok && mbar_wait(acc_full(acc), phase, abort_flag, none);
+            tc::tc_fence_after();
+            const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + acc * kPairTokens + half * 128;
+            T* const y = static_cast<T*>(p.y) + m0 * p.y_ld + channel;
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 16) {
+                uint32_t r[16];
+                tc::tmem_ld16(lanes + c0, r);
+                tc::tmem_ld_wait();
+                if (c0 == 112 && ok) {
+                    tc::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(acc_empty(acc));
+                }
+                if (c0 >= here || !has) continue;
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = ok ? scaled(static_cast<int>(r[i]), scale[c0 + i], b_scale, bias) : __int_as_float(0x7fc00000);
+                if (c0 + 16 <= here) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) from_float(y[(c0 + i) * p.y_ld], v[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c0 + i < here) from_float(y[(c0 + i) * p.y_ld], v[i]);
+                }
+            }
+            if (++acc == 2) { acc = 0; phase ^= 1u; }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::cluster_sync_all();               // neither CTA frees its tensor memory or leaves while the other may still reach it
+    if (warp == 1) {
+        tc::tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
 }
 

@@ -146,12 +146,25 @@ bool launch_product_tile(const ProductArgs& p, int device, cudaStream_t s) {
 }
 
 template <typename T>
+bool launch_product_pair(const ProductArgs& p, int device, cudaStream_t s) {
+    CUtensorMap map_a, map_b;
+    if (!make_byte_map(&map_a, p.a, p.m, p.k, p.a_ld, kPairTokens / 2) || !make_byte_map(&map_b, p.b, p.n, p.k, p.b_ld, kProdM)) return false;
+    if (cudaFuncSetAttribute(k_product_pair<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kPairSmem)) != cudaSuccess) return false;
+    const int channel_tiles = ceil_div(p.n, 2 * kProdM), token_tiles = static_cast<int>(ceil_div64(p.m, kPairTokens)), pairs = sm_count(device) / 2;
+    const int64_t tiles = static_cast<int64_t>(channel_tiles) * token_tiles;
+    launch_dependent(k_product_pair<T>, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), dim3(kPairThreads), kPairSmem, s, map_b, map_a, p,
+                     channel_tiles, token_tiles);
+    return true;
+}
+
+template <typename T>
 bool launch_product(const ProductArgs& p, int device, cudaStream_t s) {
     if (p.m <= 16) return launch_product_tile<T, 16>(p, device, s);
     if (p.m <= 32) return launch_product_tile<T, 32>(p, device, s);
     if (p.m <= 64) return launch_product_tile<T, 64>(p, device, s);
     if (p.m <= 128 || ceil_div64(p.m, 128) * ceil_div(p.n, kProdM) <= sm_count(device)) return launch_product_tile<T, 128>(p, device, s);
-    return launch_product_tile<T, 256>(p, device, s);
+    if (getenv("NOPAIR")) return launch_product_tile<T, 256>(p, device, s);
+    return launch_product_pair<T>(p, device, s);
 }
 
 }  // namespace

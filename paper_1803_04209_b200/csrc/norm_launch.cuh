@@ -45,10 +45,11 @@ bool launch_norm(const NormArgs& a, int sms, cudaStream_t s) {
     bool ok = false;
     with_team<T, V>(a.cols, a.rows > 512 || a.cols > 4096, [&](auto v, auto k, auto size) {
         constexpr int VV = decltype(v)::value, K = decltype(k)::value, SIZE = decltype(size)::value, kSize = static_cast<int>(sizeof(T));
+        const bool bias = a.post_b || a.pre_b, groups = a.gate && a.gate_rows > 1;
         const bool layer = a.post == kNormLayer || a.pre == kNormLayer;
-        const bool bias = a.post_b || a.pre_b;
-        const auto kernel = layer && bias ? k_residual_norm<T, VV, K, SIZE, true, true> : layer ? k_residual_norm<T, VV, K, SIZE, true, false>
-                            : bias ? k_residual_norm<T, VV, K, SIZE, false, true> : k_residual_norm<T, VV, K, SIZE, false, false>;
+        const auto kernel = bias && groups ? k_residual_norm<T, VV, K, SIZE, true, true, true> : bias ? k_residual_norm<T, VV, K, SIZE, true, true, false>
+                            : groups ? k_residual_norm<T, VV, K, SIZE, true, false, true>
+                            : layer  ? k_residual_norm<T, VV, K, SIZE, true, false, false> : k_residual_norm<T, VV, K, SIZE, false, false, false>;
         const int threads = SIZE ? kNormWarpThreads : team_threads(a.cols, VV * K);
         RowOperands ops{};
         const auto use = [&](const void* p, int64_t ld) { ops.o[ops.n++] = RowOperand{static_cast<const char*>(p), ld * kSize}; };
@@ -57,7 +58,7 @@ bool launch_norm(const NormArgs& a, int sms, cudaStream_t s) {
         if (a.gate && a.gate_rows == 1) use(a.gate, a.gate_ld);
         ops.row_bytes = a.cols * kSize;
         ops.slot_bytes = slot_bytes_of(ops.row_bytes, SIZE ? SIZE : threads, VV * K, kSize, VV > 1);
-        const int stage = kTeamsHere<SIZE> * ops.n * ops.slot_bytes, by_registers = 65536 / (threads * (bias ? kNormRegisters<VV, K, true> : kNormRegisters<VV, K, false>)), most = by_registers < 16 ? by_registers : 16;
+        const int stage = kTeamsHere<SIZE> * ops.n * ops.slot_bytes, by_registers = 65536 / (threads * (bias || groups ? kNormRegisters<VV, K, true> : kNormRegisters<VV, K, false>)), most = by_registers < 16 ? by_registers : 16;
         const int ctas = ceil_div(a.rows, kTeamsHere<SIZE>);
         Staging st = staging(most, stage, 0);
         if (ctas <= sms * st.per_sm) st.stages = 1, st.bytes = stage;         // a row each

@@ -158,16 +158,20 @@ __device__ __forceinline__ void add_to(Num<V> (&s)[kNums<V>], const float* p, in
     for (int i = 0; i < kNums<V>; ++i) s[i] = add(s[i], f[i]);
 }
 
-// Values as fp32 at p, or added to what is there.
+// Values as fp32 at p (16-byte aligned if V > 1), or added to what is there.
 template <int V>
 __device__ __forceinline__ void write_floats(float* p, const Num<V> (&n)[kNums<V>], bool more) {
-    float f[V];
-    if constexpr (V == 1) f[0] = n[0].v;
-    else
+    if constexpr (V == 1) {
+        *p = more ? *p + n[0].v : n[0].v;
+    } else {
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) unpack2(n[i].v, f[2 * i], f[2 * i + 1]);
-#pragma unroll
-    for (int i = 0; i < V; ++i) p[i] = more ? p[i] + f[i] : f[i];
+        for (int i = 0; i < V / 2; i += 2) {
+            ulonglong2* const q = reinterpret_cast<ulonglong2*>(p + 2 * i);
+            ulonglong2 t = make_ulonglong2(n[i].v, n[i + 1].v);
+            if (more) t = make_ulonglong2(add2(q->x, t.x), add2(q->y, t.y));
+            *q = t;
+        }
+    }
 }
 
 constexpr int kNormWarpThreads = 256;            // CTA of warp teams
@@ -200,32 +204,73 @@ template <typename T, int V, int SIZE, int K>
 __device__ __forceinline__ void take(uint32_t row_at, const Columns<SIZE, V, K>& col, int k, bool mine, Num<V> (&f)[kNums<V>]) {
     read_shared<T, V>(row_at + col(k) * static_cast<int>(sizeof(T)), (V > 1 || col.has(k)) && (SIZE == 0 || mine), f);
 }
-// A pack of the gate of a group of rows; zeros beyond the row (where an infinite gate would turn zeros into NaN).
-template <typename T, int V, int SIZE, int K>
-__device__ __forceinline__ void take_shared_gate(const T* row, const Columns<SIZE, V, K>& col, int k, Num<V> (&f)[kNums<V>]) {
-    read_global<T, V>(row + min(col(k), col.cols - V), f);
+// The gate of a group of rows, as a team that goes through the rows in their order keeps it.  Zeros beyond the row (where an infinite gate would turn
+// zeros into NaN).
+template <typename T, int V, int K>
+struct GroupGate {
+    Pack<T, V> held[K];
+    int group = -1;
+    __device__ __forceinline__ GroupGate() {      // a team without rows has zeros
 #pragma unroll
-    for (int i = 0; i < kNums<V>; ++i) f[i] = col.has(k) ? f[i] : splat<Num<V>>(0.f);
-}
+        for (int k = 0; k < K; ++k) held[k] = zero_pack<T, V>();
+    }
+    template <int SIZE>
+    __device__ __forceinline__ void turn_to(int g, const void* gate, int64_t ld, const Columns<SIZE, V, K>& col) {
+        if (g == group) return;
+        group = g;
+        const T* const row = static_cast<const T*>(gate) + g * ld;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            held[k] = zero_pack<T, V>();
+            if (!col.has(k)) continue;
+            if constexpr (V == 1) held[k].v[0] = row[col(k)];
+            else *reinterpret_cast<uint4*>(&held[k]) = __ldg(reinterpret_cast<const uint4*>(row + col(k)));
+        }
+    }
+    __device__ __forceinline__ void get(int k, Num<V> (&f)[kNums<V>]) const {
+        if constexpr (V == 1) {
+            f[0].v = to_float(held[k].v[0]);
+        } else if constexpr (sizeof(T) == 4) {
+            f[0].v = pack2(held[k].v[0], held[k].v[1]);
+            f[1].v = pack2(held[k].v[2], held[k].v[3]);
+        } else {
+            const uint4 t = *reinterpret_cast<const uint4*>(&held[k]);
+            f[0] = pair_of<T>(t.x); f[1] = pair_of<T>(t.y); f[2] = pair_of<T>(t.z); f[3] = pair_of<T>(t.w);
+        }
+    }
+};
+// Rows of team t where the teams' rows are consecutive.
+__device__ __forceinline__ int first_row_of(int t, int teams, int rows) { return rows / teams * t + min(t, rows % teams); }
+// Rows of a team.  With groups of rows they are consecutive, so that a group's gate and its gradient stay with few teams; otherwise the teams take
+// turns, so that what is read and written at a time lies together (16384 rows of 4096 bf16 values with gate: 106 us, consecutive rows 150).
+template <bool GROUPS>
+struct TeamRows {
+    int first, last, step;
+    __device__ __forceinline__ TeamRows(int t, int teams, int rows)
+        : first(GROUPS ? first_row_of(t, teams, rows) : t), last(GROUPS ? first_row_of(t + 1, teams, rows) : rows), step(GROUPS ? 1 : teams) {}
+    __device__ __forceinline__ int64_t operator()(int turn) const { return first + static_cast<int64_t>(turn) * step; }
+    __device__ __forceinline__ bool has(int turn) const { return (*this)(turn) < last; }
+};
 
 // Registers of a forward thread: with 16 values and their parameters 80, three CTAs of 256 threads per SM.
-template <int V, int K, bool BIAS>
-constexpr int kNormRegisters = V * K > 8 ? (BIAS ? 112 : 80) : (BIAS ? 80 : 64);
+template <int V, int K, bool MORE>
+constexpr int kNormRegisters = V * K > 8 ? (MORE ? 112 : 80) : (MORE ? 80 : 64);
 
 // The parameters of a thread's columns stay in its registers: in the L1, beside the operands' shared memory, there is no room for them, and every row
 // would bring them from the L2 again (4096 bf16 values with gate, 16384 rows: 152 us so; 5000 rows of 2175 fp32 values 131).
-template <typename T, int V, int K, int SIZE, bool LAYER, bool BIAS>
-__global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands) {
+template <typename T, int V, int K, int SIZE, bool LAYER, bool BIAS, bool GROUPS>
+__global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands) {
     using N = Num<V>;
     constexpr int M = kNums<V>, kBias = BIAS ? K : 1;
     CUTOFF_NORM_TEAM(a, operands)
-    const bool gate_rows = a.gate && a.gate_rows == 1;
     const int at_h = 1, at_gate = 2;
-    const int teams = gridDim.x * kTeamsHere<SIZE>, turns = ceil_div(a.rows, teams);        // as many for all teams of a warp: its shuffles take all lanes
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * kTeamsHere<SIZE> + team_here;
+    const int t = blockIdx.x * kTeamsHere<SIZE> + team_here, teams = gridDim.x * kTeamsHere<SIZE>;
+    const TeamRows<GROUPS> rows(t, teams, a.rows);
+    const int turns = ceil_div(a.rows, teams);                 // the same for all teams of a warp: its shuffles take all lanes
     bool failed = false;                          // a wait gave up: none is made after it, and nothing is asked for
     for (int s = 0; s < operands.stages; ++s)
-        if (first + static_cast<int64_t>(s) * teams < a.rows) pipe.fetch(s, first + static_cast<int64_t>(s) * teams, team);
+        if (rows.has(s)) pipe.fetch(s, rows(s), team);
+    GroupGate<T, V, GROUPS ? K : 1> group_gate;
     N post_w[K][M], pre_w[K][M], post_b[kBias][M] = {}, pre_b[kBias][M] = {};       // the block's scale is part of the first and the third
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -242,10 +287,12 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormAr
         }
     }
     for (int turn = 0; turn < turns; ++turn) {
-        const int64_t row = first + static_cast<int64_t>(turn) * teams, next = row + static_cast<int64_t>(operands.stages) * teams;
+        const int64_t row = rows(turn);
         const int stage = operands.stages == 2 ? turn & 1 : 0;
-        const bool mine = row < a.rows;           // a warp's last teams may have no row
+        const bool mine = rows.has(turn);         // a warp's teams may have a row more or less
         if (!SIZE && !mine) break;
+        if constexpr (GROUPS)
+            if (mine) group_gate.turn_to(static_cast<int>(row) / a.gate_rows, a.gate, a.gate_ld, col);
         failed = failed || (mine && !pipe.wait(turn));
         const float eps = failed ? __int_as_float(0x7fc00000) : a.eps;         // what did not arrive gives NaN
         const uint32_t x_at = pipe.template row_at<V>(stage, 0, row);
@@ -256,9 +303,7 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormAr
             for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, mine, r[k]);
             normalise<LAYER, SIZE, V, K>(r, team, col, a.post, eps, a.inv_cols);
             T* const r_row = static_cast<T*>(a.r) + row * a.r_ld;
-            const uint32_t gate_at = gate_rows ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
-            const T* const group_gate =
-                static_cast<const T*>(a.gate) + (a.gate && !gate_rows && mine ? static_cast<int64_t>(static_cast<unsigned>(row) / static_cast<unsigned>(a.gate_rows)) * a.gate_ld : 0);
+            const uint32_t gate_at = !GROUPS && a.gate ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 N t[M], x[M];
@@ -266,8 +311,8 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormAr
 #pragma unroll
                 for (int i = 0; i < M; ++i) r[k][i] = BIAS ? fma(r[k][i], post_w[k][i], post_b[BIAS ? k : 0][i]) : mul(r[k][i], post_w[k][i]);
                 if (a.gate) {
-                    if (gate_rows) take<T, V>(gate_at, col, k, mine, t);
-                    else take_shared_gate<T, V>(group_gate, col, k, t);
+                    if constexpr (GROUPS) group_gate.get(GROUPS ? k : 0, t);
+                    else take<T, V>(gate_at, col, k, mine, t);
                     gate_values<false>(t, a.gate_kind, t);
 #pragma unroll
                     for (int i = 0; i < M; ++i) r[k][i] = fma(r[k][i], t[i], x[i]);
@@ -284,7 +329,7 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormAr
         // this row's values have been used, by all of the team
         if (turn + operands.stages < turns) {
             team.sync();
-            if (!failed && next < a.rows) pipe.fetch(stage, next, team);
+            if (!failed && rows.has(turn + operands.stages)) pipe.fetch(stage, rows(turn + operands.stages), team);
         }
         if (!a.n) continue;
         normalise<LAYER, SIZE, V, K>(r, team, col, a.pre, eps, a.inv_cols);
@@ -332,9 +377,6 @@ struct NormGradArgs {
     int teams;
     int param_bytes;                              // offset in shared memory of the parameters: scale * post_w, pre_w, with BIAS scale * post_b
 };
-// Rows of team t.
-__device__ __forceinline__ int first_row_of(int t, int teams, int rows) { return rows / teams * t + min(t, rows % teams); }
-
 constexpr int kGradThreads = 512;                 // most threads of a CTA: 128 registers each
 
 // GROUPS: a gate for each group of rows, whose gradient is a sum over them.  BIAS: either norm has one, so that the plain sums are needed.
@@ -346,9 +388,10 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
     const NormArgs& a = g.f;
     CUTOFF_NORM_TEAM(a, operands)
     const int t = blockIdx.x * kTeamsHere<SIZE> + team_here;
-    const int first = first_row_of(t, g.teams, a.rows), last = first_row_of(t + 1, g.teams, a.rows);
+    const TeamRows<GROUPS> rows(t, g.teams, a.rows);
     const int turns = ceil_div(a.rows, g.teams);               // the same for all teams of a warp: its shuffles take all lanes
     constexpr int kBias = BIAS ? K : 1, kGroups = GROUPS ? K : 1;
+    GroupGate<T, V, GROUPS ? K : 1> group_gate;
     N e_hat[K][M] = {}, n_hat[K][M] = {}, e_sum[kBias][M] = {}, n_sum[kBias][M] = {}, gate_sum[kGroups][M] = {};
 
     // places of the operands in a stage
@@ -357,7 +400,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
     dependency_wait();
     bool failed = false;                          // a wait gave up: none is made after it, and nothing is asked for
     for (int s = 0; s < operands.stages; ++s)
-        if (first + s < last) pipe.fetch(s, first + s, team);
+        if (rows.has(s)) pipe.fetch(s, rows(s), team);
     // the parameters: in the L1, beside the operands, there is no room for them
     const uint32_t params = async::smem_u32(dynamic) + g.param_bytes;
     const int param_cols = team.size() * V * K;               // zeros beyond the row
@@ -373,27 +416,47 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
         }
     };
     if constexpr (SHARED) {
-        float* const p = reinterpret_cast<float*>(dynamic + g.param_bytes);
-        for (int c = threadIdx.x; c < param_cols; c += blockDim.x) {
-            const bool in = c < a.cols;
-            const float s = in ? a.scale ? a.scale[c] : 1.f : 0.f;
-            p[c] = in && a.post_w ? s * a.post_w[c] : s;
-            p[param_cols + c] = in ? a.pre_w ? a.pre_w[c] : 1.f : 0.f;
-            if constexpr (BIAS) p[2 * param_cols + c] = in && a.post_b ? s * a.post_b[c] : 0.f;
+        if (team_here == 0) {                     // a thread of the first team writes its own columns, zeros beyond the row
+            float* const p = reinterpret_cast<float*>(dynamic + g.param_bytes);
+            N w[K][M], n[K][M], b[BIAS ? K : 1][M];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+#pragma unroll
+                for (int i = 0; i < M; ++i) w[k][i] = n[k][i] = splat<N>(col.has(k) ? 1.f : 0.f);
+                if constexpr (BIAS)
+#pragma unroll
+                    for (int i = 0; i < M; ++i) b[k][i] = splat<N>(0.f);
+                if (!col.has(k)) continue;
+                multiply<V>(w[k], a.post_w, col(k));
+                multiply<V>(w[k], a.scale, col(k));
+                multiply<V>(n[k], a.pre_w, col(k));
+                if constexpr (BIAS) {
+                    add_to<V>(b[k], a.post_b, col(k));
+                    multiply<V>(b[k], a.scale, col(k));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                write_floats<V>(p + col(k), w[k], false);
+                write_floats<V>(p + param_cols + col(k), n[k], false);
+                if constexpr (BIAS) write_floats<V>(p + 2 * param_cols + col(k), b[k], false);
+            }
         }
     }
     __syncthreads();
     for (int turn = 0; turn < turns; ++turn) {
-        const int row = first + turn, stage = operands.stages == 2 ? turn & 1 : 0;
-        const bool mine = row < last;
+        const int64_t row = rows(turn);
+        const int stage = operands.stages == 2 ? turn & 1 : 0;
+        const bool mine = rows.has(turn);
         if (!SIZE && !mine) break;
         failed = failed || (mine && !pipe.wait(turn));
         const float eps = failed ? __int_as_float(0x7fc00000) : a.eps;         // what did not arrive gives NaN
-        const int group = GROUPS && mine ? row / a.gate_rows : 0;
-        const T* const group_gate = static_cast<const T*>(a.gate) + group * a.gate_ld;
+        const int group = GROUPS && mine ? static_cast<int>(row) / a.gate_rows : 0;
+        if constexpr (GROUPS)
+            if (mine) group_gate.turn_to(group, a.gate, a.gate_ld, col);
         const uint32_t gate_at = has_gate_rows ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
         const auto gate_of = [&](int k, N (&u)[M]) {
-            if constexpr (GROUPS) take_shared_gate<T, V>(group_gate, col, k, u);
+            if constexpr (GROUPS) group_gate.get(GROUPS ? k : 0, u);
             else take<T, V>(gate_at, col, k, mine, u);
         };
         N hat[K][M], d[K][M];                     // d: the whole gradient at r
@@ -513,7 +576,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
         // this row's values have been used, by all of the team
         if (turn + operands.stages < turns) {
             team.sync();
-            if (!failed && row + operands.stages < last) pipe.fetch(stage, row + operands.stages, team);
+            if (!failed && rows.has(turn + operands.stages)) pipe.fetch(stage, rows(turn + operands.stages), team);
         }
         if (a.h) {
             if (g.d_h) {
@@ -524,10 +587,10 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
             }
             if constexpr (GROUPS) {
                 // the last row of a group, or of this team: the sum is the gradient, or this team's part of it
-                if (mine && (row + 1 == last || (row + 1) / a.gate_rows != group)) {
+                if (mine && (row + 1 == rows.last || static_cast<int>(row + 1) / a.gate_rows != group)) {
                     const int64_t start = static_cast<int64_t>(group) * a.gate_rows, end = min(start + a.gate_rows, static_cast<int64_t>(a.rows));
-                    const bool whole = start >= first && end <= last;
-                    float* const part = g.gate_sums + (2 * static_cast<int64_t>(t) + (start < first ? 0 : 1)) * a.cols;
+                    const bool whole = start >= rows.first && end <= rows.last;
+                    float* const part = g.gate_sums + (2 * static_cast<int64_t>(t) + (start < rows.first ? 0 : 1)) * a.cols;
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
                         if (col.has(k)) {
@@ -591,7 +654,7 @@ constexpr int kFinishColumns = 8, kFinishSlices = 64;          // eight columns 
 // several teams had.
 template <typename T>
 __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_finish(NormFinishArgs q) {
-    __shared__ float part[4][kFinishSlices][kFinishColumns];
+    __shared__ float part[4][kFinishSlices / 4][kFinishColumns];
     const NormArgs& a = q.g.f;
     dependency_wait();
     if (static_cast<int>(blockIdx.x) >= q.column_blocks) {
@@ -623,14 +686,22 @@ __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_fi
             for (int i = 0; i < 4; ++i)
                 if (i < q.each) s[i] += q.g.sums[(static_cast<int64_t>(b) * q.each + i) * a.cols + c];
     }
+    // four slices share a warp
 #pragma unroll
-    for (int i = 0; i < 4; ++i) part[i][slice][x] = s[i];
+    for (int i = 0; i < 4; ++i) {
+        s[i] += __shfl_xor_sync(0xffffffffu, s[i], 8);
+        s[i] += __shfl_xor_sync(0xffffffffu, s[i], 16);
+    }
+    if (slice % 4 == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[i][slice / 4][x] = s[i];
     __syncthreads();
     if (slice != 0 || c >= a.cols) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         s[i] = 0.f;
-        for (int j = 0; j < kFinishSlices; ++j) s[i] += part[i][j][x];
+#pragma unroll
+        for (int j = 0; j < kFinishSlices / 4; ++j) s[i] += part[i][j][x];
     }
     const float w = a.post_w ? a.post_w[c] : 1.f, b = a.post_b ? a.post_b[c] : 0.f, scale = a.scale ? a.scale[c] : 1.f;
     if (q.d_scale) q.d_scale[c] = fmaf(w, s[0], b * s[2]);
