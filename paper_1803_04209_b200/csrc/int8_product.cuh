@@ -21,25 +21,46 @@ struct QuantizeArgs {
 };
 constexpr int kQuantizeThreads = 256;
 
-// A CTA per row.  The row is read twice; the second time it is in the L1 or L2.
+// A CTA per row.  Rows of up to KEEP packs per thread stay in registers; longer ones are read a second time, from the L2.
+constexpr int kQuantizeKeep = 4;
 template <typename T, int V>
 __global__ void __launch_bounds__(kQuantizeThreads) k_quantize_rows(QuantizeArgs a) {
     __shared__ __align__(16) float scratch[Team<0>::kScratch];
     Team<0> team(scratch);
     const T* const x = static_cast<const T*>(a.x) + blockIdx.x * a.x_ld;
     int8_t* const q = a.q + blockIdx.x * a.q_ld;
+    constexpr int kStep = kQuantizeThreads * V;
+    const int c0 = threadIdx.x * V;
     dependency_wait();
+    launch_dependents();
+    Pack<T, V> keep[kQuantizeKeep];
     uint32_t top = 0;
-    for (int c = threadIdx.x * V; c < a.cols; c += kQuantizeThreads * V) {
+#pragma unroll
+    for (int k = 0; k < kQuantizeKeep; ++k) keep[k] = c0 + k * kStep < a.cols ? load_pack<T, V>(x + c0 + k * kStep) : zero_pack<T, V>();
+#pragma unroll
+    for (int k = 0; k < kQuantizeKeep; ++k) {
+        float f[V];
+        unpack(keep[k], f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) top = max(top, magnitude_bits(f[i]));
+    }
+#pragma unroll 4
+    for (int c = c0 + kQuantizeKeep * kStep; c < a.cols; c += kStep) {
         float f[V];
         unpack(load_pack<T, V>(x + c), f);
 #pragma unroll
         for (int i = 0; i < V; ++i) top = max(top, magnitude_bits(f[i]));
     }
     const RowScale s = row_scale(team.top(top));
-    launch_dependents();
     if (threadIdx.x == 0) a.scale[blockIdx.x] = s.scale;
-    for (int c = threadIdx.x * V; c < a.cols; c += kQuantizeThreads * V) {
+#pragma unroll
+    for (int k = 0; k < kQuantizeKeep; ++k) {
+        float f[V];
+        unpack(keep[k], f);
+        if (c0 + k * kStep < a.cols) store_quantised<V>(q + c0 + k * kStep, f, s.inverse);
+    }
+#pragma unroll 4
+    for (int c = c0 + kQuantizeKeep * kStep; c < a.cols; c += kStep) {
         float f[V];
         unpack(load_pack<T, V>(x + c), f);
         store_quantised<V>(q + c, f, s.inverse);
@@ -54,42 +75,31 @@ struct ProductArgs {
     int n, k;
 };
 
-// Few rows of a: a warp per row of b, which its lanes read 16 bytes at a time, for MT rows of a.
+// One result: the same steps in the same order in every kernel.
+__device__ __forceinline__ float scaled(int total, float a_scale, float b_scale, float bias) { return fmaf(static_cast<float>(total) * a_scale, b_scale, bias); }
+
+// One row of a: a warp per row of b, which its lanes read 16 bytes at a time.
 constexpr int kDotWarps = 4;
-template <typename T, int MT>
+template <typename T>
 __global__ void __launch_bounds__(kDotWarps * 32) k_product_dot(ProductArgs p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int j = blockIdx.x * kDotWarps + warp;
-    const int64_t i0 = static_cast<int64_t>(blockIdx.y) * MT;
+    dependency_wait();
     if (j >= p.n) return;
     const int8_t* const b = p.b + static_cast<int64_t>(j) * p.b_ld;
-    int sum[MT] = {};
-    dependency_wait();
-    for (int c = lane * 16; c < p.k; c += 512) {
-        int4 w = *reinterpret_cast<const int4*>(b + c);
-        const int left = p.k - c;                // bytes beyond the row count as zeros on this side
-        if (left < 16) {
-            int* const v = &w.x;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int bytes = min(max(left - 4 * i, 0), 4);
-                v[i] = bytes == 4 ? v[i] : v[i] & ((1 << 8 * bytes) - 1);
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            if (i0 + t >= p.m) break;
-            const int4 v = *reinterpret_cast<const int4*>(p.a + (i0 + t) * p.a_ld + c);
-            sum[t] = __dp4a(v.x, w.x, __dp4a(v.y, w.y, __dp4a(v.z, w.z, __dp4a(v.w, w.w, sum[t]))));
-        }
+    const float a_scale = p.a_scale[0], b_scale = p.b_scale[j], bias = p.bias ? p.bias[j] : 0.f;
+    int sum = 0;
+    const int whole = p.k & ~15;
+#pragma unroll 8                                   // loads that wait for nothing
+    for (int c = lane * 16; c < whole; c += 512) {
+        int4 w;
+        asm volatile("ld.global.L1::no_allocate.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(b + c));
+        const int4 v = *reinterpret_cast<const int4*>(p.a + c);
+        sum = __dp4a(v.x, w.x, __dp4a(v.y, w.y, __dp4a(v.z, w.z, __dp4a(v.w, w.w, sum))));
     }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int total = __reduce_add_sync(0xffffffffu, sum[t]);
-        if (lane == 0 && i0 + t < p.m)
-            from_float(static_cast<T*>(p.y)[(i0 + t) * p.y_ld + j],
-                       fmaf(static_cast<float>(total) * p.a_scale[i0 + t], p.b_scale[j], p.bias ? p.bias[j] : 0.f));
-    }
+    if (whole + lane < p.k) sum += static_cast<int>(p.a[whole + lane]) * b[whole + lane];       // at most 15 values behind the last chunk
+    const int total = __reduce_add_sync(0xffffffffu, sum);
+    if (lane == 0) from_float(static_cast<T*>(p.y)[j], scaled(total, a_scale, b_scale, bias));
 }
 
 }  // namespace layers

@@ -5,8 +5,10 @@
 // 128-byte-swizzled K-major blocks of 128 values; what lies beyond k or the last row reads as zeros.
 //
 // k_product_tile: one tile of 128 channels x BN tokens per CTA, for few tokens or outputs.  Then the weights' bytes bound it, and what
-// counts is that all SMs stream: the K blocks of a tile are split over the CTAs of a cluster, which exchange their partial sums through
-// distributed shared memory (integers: in any order the same), each finishing its share of the tokens.
+// counts is that all SMs stream: the K blocks of a tile are split over the CTAs of a cluster, which send their partial sums to one another's
+// shared memory (integers: in any order the same) as bulk copies, each finishing its share of the tokens.  Measured, one token, 4096 x 4096 weights: split
+// in four 8.5 us, whole 12.1; 48 tokens, 8192 x 8192: 19.7 and 28.9.  Tiles of 128 tokens are never split: the exchange costs more than it gives
+// (256 tokens, 4096 x 4096: 18.8 us in two, 14.9 whole).
 //
 // k_product_pair: for many tokens and outputs.  A cluster of two CTAs works on tiles of 256 channels x 256 tokens with instructions that span both SMs
 // (cta_group::2): each CTA brings in its own 128 channels and half of the tokens, 32 KB for each 128 values of k instead of 48, and keeps the
@@ -39,22 +41,26 @@ __device__ __forceinline__ void umma_s8(uint32_t d_tmem, uint64_t a_desc, uint64
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// One result: the same steps in the same order in every kernel.
-__device__ __forceinline__ float scaled(int total, float a_scale, float b_scale, float bias) { return fmaf(static_cast<float>(total) * a_scale, b_scale, bias); }
-
 template <int BN>
 struct ProductTile {
     static constexpr int kStageBytes = kProdABytes + BN * kProdK;
     // Two CTAs per SM for few tokens, so that one streams while the other starts or ends.
-    static constexpr int kStages = BN <= 16 ? 5 : BN <= 32 ? 4 : BN <= 64 ? 3 : BN <= 128 ? 5 : 4;
+    static constexpr int kStages = BN <= 16 ? 5 : BN <= 32 ? 4 : BN <= 64 ? 3 : 6;
+    static constexpr bool kSplits = BN <= 64;
     static constexpr int kColumns = BN < 32 ? 32 : BN;                       // tensor memory comes in powers of two from 32
     static constexpr int kThreads = 192;
-    static constexpr bool kOwnExchange = BN <= 64;                           // partial sums have room of their own, or reuse the ring
-    static constexpr int kExchangeBytes = kProdM * BN * 4;
+    static constexpr int kExchangeBytes = kSplits ? kProdM * BN * 4 : 0;     // a tile's sums: they leave through the ring, which is empty by then, and arrive beside it
     static constexpr int kTailBytes = 256 + BN * 4;                          // barriers, flags; the tokens' scales
-    static_assert(kExchangeBytes <= kStages * kStageBytes || kOwnExchange, "exchange");
-    static constexpr size_t kSmemBytes = 1024 + kStages * kStageBytes + (kOwnExchange ? kExchangeBytes : 0) + kTailBytes;
+    static_assert(kExchangeBytes <= kStages * kStageBytes, "exchange");
+    static constexpr size_t kSmemBytes = 1024 + kStages * kStageBytes + kExchangeBytes + kTailBytes;
 };
+constexpr int kMostSplits = 4;                    // a CTA's share is at least four tokens
+
+// Bulk copy from this CTA's shared memory to another's, counted on a barrier there.
+__device__ __forceinline__ void bulk_to_cta(uint32_t cluster_dst, uint32_t src, uint32_t bytes, uint32_t cluster_bar) {
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(cluster_dst), "r"(src), "r"(bytes), "r"(cluster_bar) : "memory");
+}
 
 // Grid: channel tiles x token tiles x splits, a cluster of `splits` CTAs per tile.
 template <typename T, int BN>
@@ -64,16 +70,16 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u;
     uint8_t* const base = smem_raw + (ring - raw);
-    int* const exchange = reinterpret_cast<int*>(base + (Tile::kOwnExchange ? Tile::kStages * Tile::kStageBytes : 0));
-    uint8_t* const tail = base + Tile::kStages * Tile::kStageBytes + (Tile::kOwnExchange ? Tile::kExchangeBytes : 0);
+    int* const outbox = reinterpret_cast<int*>(base);
+    int* const inbox = reinterpret_cast<int*>(base + Tile::kStages * Tile::kStageBytes);
+    uint8_t* const tail = base + Tile::kStages * Tile::kStageBytes + Tile::kExchangeBytes;
     float* const token_scale = reinterpret_cast<float*>(tail + 256);
     const uint32_t bars = smem_u32(tail);
     const auto full = [&](int s) { return bars + 8 * s; };
     const auto empty = [&](int s) { return bars + 8 * (Tile::kStages + s); };
-    const uint32_t acc_full = bars + 16 * Tile::kStages;
+    const uint32_t acc_full = bars + 16 * Tile::kStages, arrived = acc_full + 8;
     volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + 16 * Tile::kStages + 16);
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(tail + 16 * Tile::kStages + 24);
-    volatile int* const peer_failed = reinterpret_cast<volatile int*>(tail + 16 * Tile::kStages + 28);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int split = static_cast<int>(blockIdx.x) % splits, tile = static_cast<int>(blockIdx.x) / splits;
@@ -89,10 +95,11 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
             mbar_init(empty(s), 1);
         }
         mbar_init(acc_full, 1);
+        mbar_init(arrived, 1);
         *abort_flag = 0;
-        *peer_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if (splits > 1) mbar_arrive_expect_tx(arrived, (splits - 1) * (Tile::kExchangeBytes / splits));      // the other CTAs' part of this one's share
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -101,7 +108,7 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (splits > 1) tc::cluster_sync_all();       // the others' flags are set up before anything reaches across
+    if (splits > 1) tc::cluster_sync_all();       // the others' barriers are set up before anything reaches across
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     dependency_wait();                            // a is an earlier kernel's, perhaps
@@ -155,8 +162,7 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
     } else {
         for (int c = threadIdx.x - 64; c < BN; c += 128) token_scale[c] = m0 + c < p.m ? p.a_scale[m0 + c] : 0.f;
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        // a split of no K blocks adds nothing (its accumulator is never written)
-        if (last > first) ok = mbar_wait(acc_full, 0u, abort_flag, none);
+        ok = mbar_wait(acc_full, 0u, abort_flag, none);
         tc::tc_fence_after();
     }
     const int quarter = warp & 3, channel = n0 + quarter * 32 + lane;
@@ -166,7 +172,7 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
     const auto put = [&](int c, float v) {
         if (has_channel && m0 + c < p.m) from_float(static_cast<T*>(p.y)[(m0 + c) * p.y_ld + channel], v);
     };
-    if (splits == 1) {
+    if (!Tile::kSplits || splits == 1) {
         if (epilogue) {
             const bool bad = !ok || *abort_flag;
 #pragma unroll 2
@@ -179,34 +185,43 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
             }
         }
     } else {
-        if constexpr (!Tile::kOwnExchange) tc::cluster_sync_all();           // all CTAs are done with their rings
-        // token c of the tile belongs to CTA c / share, which has a place for every CTA's sums: [CTA][token][channel]
-        const int share = BN / splits;
+        // Token c of the tile belongs to CTA c / share.  Sums lie as [four tokens][channel][token], so that a lane writes and reads 16 bytes beside
+        // its neighbour's and a share is one piece.
+        const int share = BN / splits, piece = share * kProdM;
         if (epilogue) {
-            if (!ok || *abort_flag)
-                for (int r = 0; r < splits; ++r)
-                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(tc::map_to_cta(smem_u32(const_cast<int*>(peer_failed)), r)), "r"(1) : "memory");
-            for (int c0 = 0; c0 < BN; c0 += 16) {
-                uint32_t r[16];
-                tc::tmem_ld16(lanes + c0, r);
-                tc::tmem_ld_wait();
+            const int lane_at = (quarter * 32 + lane) * 4;
+            const bool good = ok && !*abort_flag;
+            if (good) {
+#pragma unroll 2
+                for (int c0 = 0; c0 < BN; c0 += 16) {
+                    uint32_t r[16];
+                    tc::tmem_ld16(lanes + c0, r);
+                    tc::tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int c = c0 + i, owner = c / share;
-                    const uint32_t to = tc::map_to_cta(smem_u32(exchange + (split * share + c - owner * share) * kProdM + quarter * 32 + lane), owner);
-                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(last > first ? r[i] : 0u) : "memory");
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<uint4*>(outbox + (c0 + i) * kProdM + lane_at) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
                 }
+                fence_proxy_async();
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            const int to = threadIdx.x - 64;      // one thread per receiver; a CTA that gave up sends nothing, and the others' waits will too
+            if (good && to < splits && to != split)
+                bulk_to_cta(tc::map_to_cta(smem_u32(inbox + split * piece), to), smem_u32(outbox + to * piece), piece * 4, tc::map_to_cta(arrived, to));
+            const bool all = mbar_wait(arrived, 0u, abort_flag, none) && good;
+            for (int c = 0; c < share; c += 4) {
+                int4 total = *reinterpret_cast<const int4*>(outbox + split * piece + c * kProdM + lane_at);
+                for (int r = 0; r < splits; ++r) {
+                    if (r == split) continue;
+                    const int4 t = *reinterpret_cast<const int4*>(inbox + r * piece + c * kProdM + lane_at);
+                    total.x += t.x; total.y += t.y; total.z += t.z; total.w += t.w;
+                }
+                const int v[4] = {total.x, total.y, total.z, total.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    put(split * share + c + i, all ? scaled(v[i], token_scale[split * share + c + i], b_scale, bias) : __int_as_float(0x7fc00000));
             }
         }
-        tc::cluster_sync_all();
-        if (epilogue) {
-            const bool bad = *peer_failed;
-            for (int c = 0; c < share; ++c) {
-                int total = 0;
-                for (int r = 0; r < splits; ++r) total += exchange[(r * share + c) * kProdM + quarter * 32 + lane];
-                put(split * share + c, bad ? __int_as_float(0x7fc00000) : scaled(total, token_scale[split * share + c], b_scale, bias));
-            }
-        }
+        tc::cluster_sync_all();                   // nobody leaves while its sums are on their way
     }
     tc::tc_fence_before();
     __syncthreads();

@@ -118,17 +118,21 @@ bool make_byte_map(CUtensorMap* map, const int8_t* base, int64_t rows, int64_t c
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles of BN tokens x 128 outputs.
+int64_t product_tiles(const ProductArgs& p, int tokens) { return ceil_div64(p.m, tokens) * ceil_div(p.n, kProdM); }
+
 template <typename T, int BN>
 bool launch_product_tile(const ProductArgs& p, int device, cudaStream_t s) {
     using Tile = ProductTile<BN>;
     CUtensorMap map_a, map_b;
     if (!make_byte_map(&map_a, p.a, p.m, p.k, p.a_ld, BN) || !make_byte_map(&map_b, p.b, p.n, p.k, p.b_ld, kProdM)) return false;
     if (cudaFuncSetAttribute(k_product_tile<T, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Tile::kSmemBytes)) != cudaSuccess) return false;
-    const int64_t token_tiles = ceil_div64(p.m, BN), tiles = token_tiles * ceil_div(p.n, kProdM);
-    // K blocks of a tile are split until the GPU is filled, but no CTA gets less than two of them
-    const int sms = sm_count(device), blocks = ceil_div(p.k, kProdK), want = BN <= 64 ? sms * 3 / 2 : sms * 3 / 4;
+    const int64_t token_tiles = ceil_div64(p.m, BN), tiles = product_tiles(p, BN);
+    // the K blocks of a tile are split until three CTAs for two SMs are there, but no CTA gets less than two blocks
+    const int blocks = ceil_div(p.k, kProdK);
     int splits = 1;
-    while (splits < 8 && tiles * splits < want && blocks >= 4 * splits) splits *= 2;
+    if (Tile::kSplits)
+        while (splits < kMostSplits && tiles * splits * 2 < sm_count(device) * 3 && blocks >= 4 * splits) splits *= 2;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(tiles * splits));
     cfg.blockDim = dim3(Tile::kThreads);
@@ -159,11 +163,20 @@ bool launch_product_pair(const ProductArgs& p, int device, cudaStream_t s) {
 
 template <typename T>
 bool launch_product(const ProductArgs& p, int device, cudaStream_t s) {
-    if (p.m <= 16) return launch_product_tile<T, 16>(p, device, s);
-    if (p.m <= 32) return launch_product_tile<T, 32>(p, device, s);
-    if (p.m <= 64) return launch_product_tile<T, 64>(p, device, s);
-    if (p.m <= 128 || ceil_div64(p.m, 128) * ceil_div(p.n, kProdM) <= sm_count(device)) return launch_product_tile<T, 128>(p, device, s);
-    if (getenv("NOPAIR")) return launch_product_tile<T, 256>(p, device, s);
+    // One token: as its products are few, the vector unit's dot products follow the weights (4096 x 4096 6.1 us, tensor-core tiles 8.5; 8192 x 8192
+    // 15.4 and 16.0); with two they do not any more (11.3, 8.5).
+    if (p.m == 1) {
+        launch_dependent(k_product_dot<T>, dim3(ceil_div(p.n, kDotWarps)), dim3(kDotWarps * 32), 0, s, p);
+        return true;
+    }
+    // The fewest tokens per tile that hold them all, or whose tiles, split in four, are resident at a time: the latency of the K blocks bounds a CTA, and
+    // what a second tile reads again comes from the L2 (300 x 512 x 8192: 32 tokens 12 us, 64 13, 128 21).  Then whole tiles of 128 tokens, one per
+    // SM (512 x 4096 x 4096 16.3 us, pairs of SMs 17.9), then pairs (1000 x 4096 x 4096 18.0 us, tiles of 128 tokens 28.6).
+    const int64_t sms = sm_count(device), resident = 2 * sms / kMostSplits;
+    if (p.m <= 16 || product_tiles(p, 16) <= resident) return launch_product_tile<T, 16>(p, device, s);
+    if (p.m <= 32 || product_tiles(p, 32) <= resident) return launch_product_tile<T, 32>(p, device, s);
+    if (p.m <= 64 || product_tiles(p, 64) <= resident) return launch_product_tile<T, 64>(p, device, s);
+    if (product_tiles(p, 128) <= sms) return launch_product_tile<T, 128>(p, device, s);
     return launch_product_pair<T>(p, device, s);
 }
 

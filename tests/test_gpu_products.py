@@ -58,8 +58,9 @@ def _bound(want, total, a_scale, b_scale, bias, dt):
 
 # one token to many, both sides of every border between kernels and tiles, inner lengths that end inside a chunk of 16, 32, 64 and 128
 SIZES = [(1, 1, 1), (1, 8, 16), (2, 5, 17), (1, 300, 4096), (3, 129, 130), (8, 128, 512), (9, 64, 100), (16, 256, 128), (17, 200, 1000), (33, 130, 33),
-         (64, 1024, 256), (65, 127, 129), (128, 128, 128), (129, 257, 640), (200, 513, 1001), (256, 256, 2048), (257, 600, 96), (300, 8, 48), (1000, 130, 272),
-         (2, 2048, 8192), (48, 640, 8192), (100, 2175, 513), (1024, 1024, 512)]
+         (64, 1024, 256), (64, 9600, 384), (65, 127, 129), (128, 128, 128), (129, 257, 640), (200, 513, 1001), (256, 256, 2048), (257, 600, 96), (300, 8, 48), (1000, 130, 272),
+         (2, 2048, 8192), (48, 640, 8192), (100, 2175, 513), (1024, 1024, 512), (300, 512, 4096), (200, 5000, 640),
+         (1300, 2300, 200), (4000, 2000, 129)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
