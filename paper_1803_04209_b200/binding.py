@@ -139,8 +139,8 @@ def load_library(path: str | None = None) -> C.CDLL:
         "cutoff_sorted_row_sums_static": (C.c_int, [C.c_int, vp, C.c_int64, C.c_int32, C.c_int32, vp, vp]),
         "cutoff_dropout": (C.c_int, [C.c_int, C.c_int32, C.c_int64, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, C.c_double, C.c_uint64,
                                      C.c_uint32, C.c_uint32, C.c_int64, vp]),
-        "cutoff_residual_norm": (C.c_int, [C.c_int, C.POINTER(NormLayer), vp, C.c_int64, vp, C.c_int64, vp, vp]),
-        "cutoff_residual_norm_grad": (C.c_int, [C.c_int, C.POINTER(NormLayer), vp, C.c_int64, vp, C.c_int64, C.POINTER(NormGrads), vp, C.c_size_t, vp]),
+        "cutoff_residual_norm": (C.c_int, [C.c_int, vp, vp, C.c_int64, vp, C.c_int64, vp, vp]),
+        "cutoff_residual_norm_grad": (C.c_int, [C.c_int, vp, vp, C.c_int64, vp, C.c_int64, vp, vp, C.c_size_t, vp]),
         "cutoff_residual_norm_grad_workspace_bytes": (C.c_int64, [C.c_int64, C.c_int32]),
         "cutoff_quantize_rows": (C.c_int, [C.c_int, C.c_int32, C.c_int64, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp, vp]),
         "cutoff_quantized_product": (C.c_int, [C.c_int, C.c_int64, C.c_int32, C.c_int32, vp, C.c_int64, vp, vp, C.c_int64, vp, vp, C.c_int32, vp,
@@ -550,44 +550,70 @@ class Quantized(NamedTuple):
     scale: object                   # fp32 [rows]
 
 
-def _type_of(t) -> int:
-    import torch
-    code = {torch.float32: TYPE_FP32, torch.float16: TYPE_FP16, torch.bfloat16: TYPE_BF16}.get(t.dtype)
+# The two structures of the norm calls as bytes: a tenth of the time that filling ctypes fields takes.
+_NORM_LAYER = struct.Struct("qiiPqPqPqqiiifPPPPP")
+_NORM_GRADS = struct.Struct("PqPqPqPPPPP")
+assert _NORM_LAYER.size == C.sizeof(NormLayer) and _NORM_GRADS.size == C.sizeof(NormGrads)
+_torch = _raw_stream = None
+_type_codes = {}
+
+
+def _load_torch():
+    """torch, once, and the codes of the types that the layer operators take."""
+    global _torch, _type_codes, _raw_stream
+    if _torch is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _type_codes = {torch.float32: TYPE_FP32, torch.float16: TYPE_FP16, torch.bfloat16: TYPE_BF16}
+        _torch = torch
+    return _torch
+
+
+def _type_of(dtype) -> int:
+    code = _type_codes.get(dtype)
     if code is None:
-        raise ValueError(f"expected a tensor of fp32, fp16 or bf16 values, not {t.dtype}")
+        raise ValueError(f"expected fp32, fp16 or bf16 values, not {dtype}")
     return code
 
 
-def _matrix(t, what: str, like=None, rows: int | None = None, dtype=None):
-    """(address, leading dimension) of a matrix; `like`: the matrix whose device, columns, type and (unless `rows` is given) rows it has to have."""
-    if t is None:
-        return None, 0
-    if t.dim() != 2 or not t.is_cuda or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: expected a CUDA matrix [rows, columns] with contiguous rows")
-    if like is not None and (t.device != like.device or t.shape[1] != like.shape[1] or t.shape[0] != (like.shape[0] if rows is None else rows) or
-                             t.dtype != (like.dtype if dtype is None else dtype)):
-        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device} does not fit {like.dtype} {tuple(like.shape)} on {like.device}")
-    n, cols = t.shape
-    if n <= 1:
-        # the distance to a row that there is not may be anything, and so may the address of no rows (torch says 0, which would read as "absent")
-        return t.data_ptr() or 16, max(t.stride(0), cols)
-    if t.stride(0) < cols:
+def _matrix(t, what: str):
+    """(address, leading dimension, rows, columns, device, type) of a CUDA matrix with contiguous rows."""
+    shape, device = t.shape, t.get_device()
+    if len(shape) != 2 or device < 0 or shape[1] < 1:
+        raise ValueError(f"{what}: expected a CUDA matrix [rows, columns]")
+    rows, cols = shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what}: expected contiguous rows")
+    if rows <= 1:                   # the distance to a row that there is not may be anything
+        ld = max(ld, cols)
+    elif ld < cols:
         raise ValueError(f"{what}: rows overlap")
-    return t.data_ptr(), t.stride(0)
+    # the address of no rows may be anything too (torch says 0, which would read as "absent")
+    return t.data_ptr() or 16, ld, rows, cols, device, t.dtype
 
 
-def _vector(t, what: str, like, n: int):
-    import torch
+def _same(t, what: str, rows: int, cols: int, device: int, dtype):
+    """(address, leading dimension) of a matrix that has to have this shape, device and type; None is none."""
     if t is None:
-        return None
-    if t.dtype != torch.float32 or t.device != like.device or tuple(t.shape) != (n,) or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous fp32 vector of {n} values on {like.device}")
+        return 0, 0
+    at, ld, r, c, d, kind = _matrix(t, what)
+    if r != rows or c != cols or d != device or kind is not dtype:
+        raise ValueError(f"{what}: {kind} [{r}, {c}] on cuda:{d} where {dtype} [{rows}, {cols}] on cuda:{device} is expected")
+    return at, ld
+
+
+def _vector(t, what: str, n: int, device: int) -> int:
+    if t is None:
+        return 0
+    if t.dtype is not _torch.float32 or t.get_device() != device or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous fp32 vector of {n} values on cuda:{device}")
     return t.data_ptr() or 16
 
 
-def _stream_of(t):
-    import torch
-    return t.device.index, torch.cuda.current_stream(t.device).cuda_stream
+def _current_stream(device: int) -> int:
+    """torch's current stream on a device (its handle without the Stream object around it, where this torch has that: 0.1 us instead of 1.4)."""
+    return _raw_stream(device) if _raw_stream else _torch.cuda.current_stream(device).cuda_stream
 
 
 def dropout(x, p: float, seed: int, step: int = 0, noise_stream: int = STREAM_DROPOUT, first_row: int = 0, residual=None, out=None):
@@ -595,34 +621,35 @@ def dropout(x, p: float, seed: int, step: int = 0, noise_stream: int = STREAM_DR
 
     The gradient with respect to x is dropout(gradient of the result, p, seed, step, noise_stream, first_row); that with respect to the
     residual is the gradient of the result.  p counts in steps of 2^-16.  out may be x or residual."""
-    import torch
-    lib = load_library()
-    xp, x_ld = _matrix(x, "x")
+    torch, lib = _load_torch(), load_library()
+    xp, x_ld, rows, cols, device, dtype = _matrix(x, "x")
+    code = _type_of(dtype)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    rp, r_ld = _matrix(residual, "residual", x)
-    op, o_ld = _matrix(out, "out", x)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    rp, r_ld = _same(residual, "residual", rows, cols, device, dtype)
+    op, o_ld = _same(out, "out", rows, cols, device, dtype)
     if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= noise_stream < 1 << 32):
         raise ValueError("seed has 64 bits, step and noise_stream 32")
-    device, stream = _stream_of(x)
-    rc = lib.cutoff_dropout(device, _type_of(x), x.shape[0], x.shape[1], xp, x_ld, rp, r_ld, op, o_ld, p, seed, step, noise_stream, first_row, stream)
+    rc = lib.cutoff_dropout(device, code, rows, cols, xp, x_ld, rp, r_ld, op, o_ld, p, seed, step, noise_stream, first_row, _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_dropout")
     return out
 
 
 def _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps):
+    """(the layer as bytes, rows, columns, device, type)"""
     if post not in NORMS or pre not in NORMS or gate_kind not in GATES:
         raise ValueError(f"norms: {list(NORMS)}, gates: {list(GATES)}")
     if gate_rows < 1:
         raise ValueError("gate_rows is at least 1")
-    xp, x_ld = _matrix(x, "x")
-    hp, h_ld = _matrix(h, "h", x)
-    rows, cols = x.shape
-    gp, g_ld = _matrix(gate, "gate", x, rows=-(-rows // gate_rows))
-    return NormLayer(rows, cols, _type_of(x), xp, x_ld, hp, h_ld, gp, g_ld, gate_rows, GATES[gate_kind], NORMS[post], NORMS[pre], eps,
-                     _vector(scale, "scale", x, cols), _vector(post_weight, "post_weight", x, cols), _vector(post_bias, "post_bias", x, cols),
-                     _vector(pre_weight, "pre_weight", x, cols), _vector(pre_bias, "pre_bias", x, cols))
+    xp, x_ld, rows, cols, device, dtype = _matrix(x, "x")
+    hp, h_ld = _same(h, "h", rows, cols, device, dtype)
+    gp, g_ld = _same(gate, "gate", -(-rows // gate_rows), cols, device, dtype)
+    layer = _NORM_LAYER.pack(rows, cols, _type_of(dtype), xp, x_ld, hp, h_ld, gp, g_ld, gate_rows, GATES[gate_kind], NORMS[post], NORMS[pre], eps,
+                             _vector(scale, "scale", cols, device), _vector(post_weight, "post_weight", cols, device),
+                             _vector(post_bias, "post_bias", cols, device), _vector(pre_weight, "pre_weight", cols, device),
+                             _vector(pre_bias, "pre_bias", cols, device))
+    return layer, rows, cols, device, dtype
 
 
 def residual_norm(x, h=None, gate=None, gate_rows: int = 1, gate_kind: str = "linear", scale=None, post: str | None = "rms", post_weight=None,
@@ -633,22 +660,18 @@ def residual_norm(x, h=None, gate=None, gate_rows: int = 1, gate_kind: str = "li
     x, h [rows, cols]; gate [ceil(rows / gate_rows), cols]; post, pre: "rms", "layer" or None, with weights and biases [cols].  Without h there is no
     block before: r is x.  With want_norm=False n is None.  With quantize=True n is a Quantized of 8-bit rows, as quantized_product takes them.
     residual_out and norm_out may be x or h."""
-    import torch
-    lib = load_library()
-    layer = _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps)
-    rows, cols = x.shape
+    torch, lib = _load_torch(), load_library()
+    layer, rows, cols, device, dtype = _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps)
     r, rp, r_ld, n, np_, n_ld, sp = x, None, 0, None, None, 0, None
     if h is not None:
-        r = torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual_out is None else residual_out
-        rp, r_ld = _matrix(r, "residual_out", x)
+        r = torch.empty_like(x, memory_format=torch.contiguous_format) if residual_out is None else residual_out
+        rp, r_ld = _same(r, "residual_out", rows, cols, device, dtype)
     if want_norm and quantize:
-        n = _empty_quantized(rows, cols, x.device)
-        np_, n_ld, sp = n.values.data_ptr() or 16, (cols + 15) // 16 * 16, n.scale.data_ptr() or 16
+        n, np_, n_ld, sp = _empty_quantized(x, rows, cols)
     elif want_norm:
-        n = torch.empty(x.shape, dtype=x.dtype, device=x.device) if norm_out is None else norm_out
-        np_, n_ld = _matrix(n, "norm_out", x)
-    device, stream = _stream_of(x)
-    rc = lib.cutoff_residual_norm(device, C.byref(layer), rp, r_ld, np_, n_ld, sp, stream)
+        n = torch.empty_like(x, memory_format=torch.contiguous_format) if norm_out is None else norm_out
+        np_, n_ld = _same(n, "norm_out", rows, cols, device, dtype)
+    rc = lib.cutoff_residual_norm(device, layer, rp, r_ld, np_, n_ld, sp, _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_residual_norm")
     return r, n
@@ -659,46 +682,41 @@ def residual_norm_grad(x, h, d_residual, d_norm, gate=None, gate_rows: int = 1, 
     """The gradients of residual_norm's inputs ("x", and of "h", "gate", "scale", "post_weight", "post_bias", "pre_weight", "pre_bias" those that
     there are), given those of a loss with respect to r and n (either may be None).  x and h are the forward pass's inputs; nothing of its
     results is needed."""
-    import torch
-    lib = load_library()
-    layer = _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps)
-    rows, cols = x.shape
-    rp, r_ld = _matrix(d_residual, "d_residual", x)
-    np_, n_ld = _matrix(d_norm, "d_norm", x)
-    out = {"x": torch.empty(x.shape, dtype=x.dtype, device=x.device)}
-    for name, t in (("h", h), ("gate", gate), ("scale", scale), ("post_weight", post_weight), ("post_bias", post_bias), ("pre_weight", pre_weight),
+    torch, lib = _load_torch(), load_library()
+    layer, rows, cols, device, dtype = _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps)
+    rp, r_ld = _same(d_residual, "d_residual", rows, cols, device, dtype)
+    np_, n_ld = _same(d_norm, "d_norm", rows, cols, device, dtype)
+    out, at = {}, []
+    for name, t in (("x", x), ("h", h), ("gate", gate), ("scale", scale), ("post_weight", post_weight), ("post_bias", post_bias), ("pre_weight", pre_weight),
                     ("pre_bias", pre_bias)):
-        if t is not None:
-            out[name] = torch.empty(t.shape, dtype=t.dtype, device=x.device)
-
-    def at(name):
-        return out[name].data_ptr() or 16 if name in out else None
-    grads = NormGrads(at("x"), cols, at("h"), cols, at("gate"), cols, at("scale"), at("post_weight"), at("post_bias"), at("pre_weight"), at("pre_bias"))
-    need = lib.cutoff_residual_norm_grad_workspace_bytes(rows, cols)
-    ws = torch.empty(max(need, 256), dtype=torch.uint8, device=x.device)
-    device, stream = _stream_of(x)
-    rc = lib.cutoff_residual_norm_grad(device, C.byref(layer), rp, r_ld, np_, n_ld, C.byref(grads), ws.data_ptr(), ws.numel(), stream)
+        if t is None:
+            at.append(0)
+        else:
+            out[name] = g = torch.empty_like(t, memory_format=torch.contiguous_format)
+            at.append(g.data_ptr() or 16)
+    grads = _NORM_GRADS.pack(at[0], cols, at[1], cols, at[2], cols, *at[3:])
+    ws = torch.empty(max(lib.cutoff_residual_norm_grad_workspace_bytes(rows, cols), 256), dtype=torch.uint8, device=x.device)
+    rc = lib.cutoff_residual_norm_grad(device, layer, rp or None, r_ld, np_ or None, n_ld, grads, ws.data_ptr(), ws.numel(), _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_residual_norm_grad")
     return out
 
 
-def _empty_quantized(rows: int, cols: int, device) -> Quantized:
-    import torch
-    values = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)
-    return Quantized(values[:, :cols], torch.empty(rows, dtype=torch.float32, device=device))
+def _empty_quantized(like, rows: int, cols: int):
+    """(Quantized, address of its values, their leading dimension, address of its scales)"""
+    ld = (cols + 15) // 16 * 16
+    values, scale = like.new_empty((rows, ld), dtype=_torch.int8), like.new_empty(rows, dtype=_torch.float32)
+    return Quantized(values[:, :cols] if ld > cols else values, scale), values.data_ptr() or 16, ld, scale.data_ptr() or 16
 
 
 def quantize_rows(x) -> Quantized:
     """8-bit integers of each row of x and their scale (largest magnitude / 127): the tokens of a product, or once its weights [outputs, inputs]."""
     lib = load_library()
-    xp, x_ld = _matrix(x, "x")
-    rows, cols = x.shape
-    q = _empty_quantized(rows, cols, x.device)
-    if rows == 0:
-        return q
-    device, stream = _stream_of(x)
-    rc = lib.cutoff_quantize_rows(device, _type_of(x), rows, cols, xp, x_ld, q.values.data_ptr(), (cols + 15) // 16 * 16, q.scale.data_ptr(), stream)
+    _load_torch()
+    xp, x_ld, rows, cols, device, dtype = _matrix(x, "x")
+    code = _type_of(dtype)
+    q, qp, q_ld, sp = _empty_quantized(x, rows, cols)
+    rc = lib.cutoff_quantize_rows(device, code, rows, cols, xp, x_ld, qp, q_ld, sp, _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_quantize_rows")
     return q
@@ -708,22 +726,22 @@ def quantized_product(a, b, bias=None, dtype=None, out=None):
     """a b^T of two Quantized (or pairs of int8 rows and fp32 scales): a [m, k] tokens, b [n, k] weights; plus bias [n].
 
     Returns [m, n] of `dtype` (bf16 if neither it nor `out` is given).  The integer sums are exact.  Rows of a and b start on 16-byte boundaries."""
-    import torch
-    lib = load_library()
+    torch, lib = _load_torch(), load_library()
     (av, a_scale), (bv, b_scale) = a, b
-    ap, a_ld = _matrix(av, "a")
-    bp, b_ld = _matrix(bv, "b", av, rows=bv.shape[0])
-    if av.dtype != torch.int8:
+    ap, a_ld, m, k, device, kind = _matrix(av, "a")
+    if kind is not torch.int8:
         raise ValueError("expected rows of int8 values")
-    m, n, k = av.shape[0], bv.shape[0], av.shape[1]
+    n = bv.shape[0]
+    bp, b_ld = _same(bv, "b", n, k, device, kind)
     if out is None:
-        out = torch.empty((m, n), dtype=dtype or torch.bfloat16, device=av.device)
-    elif tuple(out.shape) != (m, n) or out.device != av.device or (dtype is not None and out.dtype != dtype):
-        raise ValueError(f"out: expected [{m}, {n}] on {av.device}")
-    op, o_ld = _matrix(out, "out")
-    device, stream = _stream_of(av)
-    rc = lib.cutoff_quantized_product(device, m, n, k, ap, a_ld, _vector(a_scale, "a's scale", av, m), bp, b_ld, _vector(b_scale, "b's scale", av, n),
-                                      _vector(bias, "bias", av, n), _type_of(out), op, o_ld, stream)
+        code = _type_of(dtype or torch.bfloat16)
+        out = av.new_empty((m, n), dtype=dtype or torch.bfloat16)
+        op, o_ld = out.data_ptr() or 16, n
+    else:
+        code = _type_of(out.dtype)
+        op, o_ld = _same(out, "out", m, n, device, dtype or out.dtype)
+    rc = lib.cutoff_quantized_product(device, m, n, k, ap, a_ld, _vector(a_scale, "a's scale", m, device), bp, b_ld,
+                                      _vector(b_scale, "b's scale", n, device), _vector(bias, "bias", n, device), code, op, o_ld, _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_quantized_product")
     return out
