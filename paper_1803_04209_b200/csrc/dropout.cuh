@@ -30,10 +30,10 @@ struct DropoutArgs {
 
 constexpr int kDropoutThreads = 256;
 
-// LX: lanes that share a row (each with eight columns), 32 / LX rows per warp.  V: values per access.  U: rows of a thread on
-// their way at a time.
-template <typename T, int V, int LX, int U>
-__global__ void __launch_bounds__(kDropoutThreads) k_dropout(DropoutArgs a) {
+// LX: lanes that share a row (each with eight columns), 32 / LX rows per warp.  V: values per access.  U: rows of a thread on their way at a time.
+// ADD: there is a residual.
+template <typename T, int V, int LX, int U, bool ADD>
+__global__ void __launch_bounds__(kDropoutThreads, 3) k_dropout(DropoutArgs a) {
     constexpr int kRowsPerWarp = 32 / LX;
     const int lane = threadIdx.x & 31, l = lane % LX;
     const int64_t warp = (static_cast<int64_t>(blockIdx.x) * kDropoutThreads + threadIdx.x) >> 5, warps = static_cast<int64_t>(gridDim.x) * (kDropoutThreads / 32);
@@ -43,25 +43,29 @@ __global__ void __launch_bounds__(kDropoutThreads) k_dropout(DropoutArgs a) {
     const int64_t stride = each * kRowsPerWarp;
     const int c0 = (tile * LX + l) * 8;                   // this lane's columns, as the generator counts them
     const uint4 column = philox_column(static_cast<uint32_t>(c0 >> 3), a.stream, a.step, a.key.seed_lo, a.key.seed_hi);
-    const T* const x = static_cast<const T*>(a.x);
-    const T* const res = static_cast<const T*>(a.residual);
-    T* const y = static_cast<T*>(a.y);
 
     // Values of this lane: with whole packs the eight columns from c0; with single values columns l, LX + l, ... of the tile, so that
     // a warp's accesses are consecutive, and the kept bits come from the lanes that drew them.
     constexpr int kPacks = V == 1 ? 8 : 8 / V;
-    const auto column_of = [&](int k) { return V == 1 ? tile * LX * 8 + k * LX + l : c0 + k * V; };
+    constexpr int kApart = V == 1 ? LX : V;
+    const int first = V == 1 ? tile * LX * 8 + l : c0;
+    bool has[kPacks];
+#pragma unroll
+    for (int k = 0; k < kPacks; ++k) has[k] = first + k * kApart < a.cols;
+    const T* const x = static_cast<const T*>(a.x) + first;
+    const T* const res = static_cast<const T*>(a.residual) + first;
+    T* const y = static_cast<T*>(a.y) + first;
 
-    for (int64_t row0 = warp / a.tiles * kRowsPerWarp + lane / LX; row0 - lane / LX < a.rows; row0 += U * stride) {
-        Pack<T, V> in[U][kPacks], add[U][kPacks];
+    const auto rows_from = [&](int64_t row0, auto all) {  // all: the U rows are there
+        Pack<T, V> in[U][kPacks], add[ADD ? U : 1][kPacks];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = row0 + u * stride;
 #pragma unroll
             for (int k = 0; k < kPacks; ++k) {
-                const bool ok = row < a.rows && column_of(k) < a.cols;
-                in[u][k] = ok ? load_pack<T, V>(x + row * a.x_ld + column_of(k)) : zero_pack<T, V>();
-                if (res) add[u][k] = ok ? load_pack<T, V>(res + row * a.residual_ld + column_of(k)) : zero_pack<T, V>();
+                const bool ok = (decltype(all)::value || row < a.rows) && has[k];
+                in[u][k] = ok ? load_pack<T, V>(x + row * a.x_ld + k * kApart) : zero_pack<T, V>();
+                if constexpr (ADD) add[u][k] = ok ? load_pack<T, V>(res + row * a.residual_ld + k * kApart) : zero_pack<T, V>();
             }
         }
 #pragma unroll
@@ -86,7 +90,7 @@ __global__ void __launch_bounds__(kDropoutThreads) k_dropout(DropoutArgs a) {
             for (int k = 0; k < kPacks; ++k) {
                 float f[V], g[V];
                 unpack(in[u][k], f);
-                if (res) {
+                if constexpr (ADD) {
                     unpack(add[u][k], g);
 #pragma unroll
                     for (int i = 0; i < V; ++i) f[i] = keep[k * V + i] ? fmaf(f[i], a.scale, g[i]) : g[i];
@@ -94,10 +98,14 @@ __global__ void __launch_bounds__(kDropoutThreads) k_dropout(DropoutArgs a) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) f[i] = keep[k * V + i] ? f[i] * a.scale : 0.f;
                 }
-                if (row < a.rows && column_of(k) < a.cols) store_pack<T, V>(y + row * a.y_ld + column_of(k), f);
+                if ((decltype(all)::value || row < a.rows) && has[k]) store_pack<T, V>(y + row * a.y_ld + k * kApart, f);
             }
         }
-    }
+    };
+    // the warp's first row decides for the warp: its shuffles take all lanes
+    int64_t row0 = warp / a.tiles * kRowsPerWarp;
+    for (; row0 + (U - 1) * stride + kRowsPerWarp <= a.rows; row0 += U * stride) rows_from(row0 + lane / LX, std::true_type{});
+    for (; row0 < a.rows; row0 += U * stride) rows_from(row0 + lane / LX, std::false_type{});
 }
 
 }  // namespace layers
