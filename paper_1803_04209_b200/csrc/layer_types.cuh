@@ -136,24 +136,33 @@ __device__ __forceinline__ F2 pair_of(uint32_t w) {
         return F2{pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u))};
     }
 }
-// V values of type T at a shared-memory address (16-byte aligned if V > 1), or zeros.  Predicates and not branches, here and in write_global: a
-// branch for each pack costs more than the pack's arithmetic.
-template <typename T, int V>
-__device__ __forceinline__ void read_shared(uint32_t at, bool ok, Num<V> (&f)[kNums<V>]) {
-    const int p = ok;
-    if constexpr (V == 1 && sizeof(T) == 4) {
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\tmov.f32 %0, 0f00000000;\n\t@p ld.shared.f32 %0, [%1];\n\t}" : "=f"(f[0].v) : "r"(at), "r"(p) : "memory");
+// V values of type T at a shared-memory address (16-byte aligned if V > 1); with CHECK zeros unless column < columns.  Predicates and not branches, here and
+// in write_global, and the comparison beside them: a branch for each pack costs more than the pack's arithmetic.
+template <typename T, int V, bool CHECK>
+__device__ __forceinline__ void read_shared(uint32_t at, int column, int columns, Num<V> (&f)[kNums<V>]) {
+    if constexpr (!CHECK) {
+        static_assert(V > 1, "single values are checked");
+        if constexpr (sizeof(T) == 4) {
+            asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f[0].v), "=l"(f[1].v) : "r"(at) : "memory");
+        } else {
+            uint32_t w[4];
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = pair_of<T>(w[i]);
+        }
+    } else if constexpr (V == 1 && sizeof(T) == 4) {
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %2, %3;\n\tmov.f32 %0, 0f00000000;\n\t@p ld.shared.f32 %0, [%1];\n\t}" : "=f"(f[0].v) : "r"(at), "r"(column), "r"(columns) : "memory");
     } else if constexpr (V == 1) {
         unsigned short u;
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\tmov.u16 %0, 0;\n\t@p ld.shared.u16 %0, [%1];\n\t}" : "=h"(u) : "r"(at), "r"(p) : "memory");
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %2, %3;\n\tmov.u16 %0, 0;\n\t@p ld.shared.u16 %0, [%1];\n\t}" : "=h"(u) : "r"(at), "r"(column), "r"(columns) : "memory");
         f[0].v = to_float(*reinterpret_cast<const T*>(&u));
     } else if constexpr (sizeof(T) == 4) {
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %3, 0;\n\tmov.b64 %0, 0;\n\tmov.b64 %1, 0;\n\t@p ld.shared.v2.b64 {%0, %1}, [%2];\n\t}"
-                     : "=l"(f[0].v), "=l"(f[1].v) : "r"(at), "r"(p) : "memory");
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %3, %4;\n\tmov.b64 %0, 0;\n\tmov.b64 %1, 0;\n\t@p ld.shared.v2.b64 {%0, %1}, [%2];\n\t}"
+                     : "=l"(f[0].v), "=l"(f[1].v) : "r"(at), "r"(column), "r"(columns) : "memory");
     } else {
         uint32_t w[4];
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t@p ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at), "r"(p) : "memory");
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %5, %6;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t@p ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at), "r"(column), "r"(columns) : "memory");
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = pair_of<T>(w[i]);
     }
@@ -185,19 +194,20 @@ __device__ __forceinline__ void read_global(const T* p, Num<V> (&f)[kNums<V>]) {
         f[0] = pair_of<T>(t.x); f[1] = pair_of<T>(t.y); f[2] = pair_of<T>(t.z); f[3] = pair_of<T>(t.w);
     }
 }
+// V values at p + column, if column < columns.
 template <typename T, int V>
-__device__ __forceinline__ void write_global(T* at, bool ok, const Num<V> (&n)[kNums<V>]) {
-    const int p = ok;
+__device__ __forceinline__ void write_global(T* p, int column, int columns, const Num<V> (&n)[kNums<V>]) {
+    T* const at = p + column;
     if constexpr (V == 1) {
         T v;
         from_float(v, n[0].v);
         if constexpr (sizeof(T) == 4) {
-            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p st.global.f32 [%0], %1;\n\t}" ::"l"(at), "f"(n[0].v), "r"(p) : "memory");
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %2, %3;\n\t@p st.global.f32 [%0], %1;\n\t}" ::"l"(at), "f"(n[0].v), "r"(column), "r"(columns) : "memory");
         } else {
-            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p st.global.u16 [%0], %1;\n\t}" ::"l"(at), "h"(*reinterpret_cast<const unsigned short*>(&v)), "r"(p) : "memory");
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %2, %3;\n\t@p st.global.u16 [%0], %1;\n\t}" ::"l"(at), "h"(*reinterpret_cast<const unsigned short*>(&v)), "r"(column), "r"(columns) : "memory");
         }
     } else if constexpr (sizeof(T) == 4) {
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %3, 0;\n\t@p st.global.v2.b64 [%0], {%1, %2};\n\t}" ::"l"(at), "l"(n[0].v), "l"(n[1].v), "r"(p) : "memory");
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %3, %4;\n\t@p st.global.v2.b64 [%0], {%1, %2};\n\t}" ::"l"(at), "l"(n[0].v), "l"(n[1].v), "r"(column), "r"(columns) : "memory");
     } else {
         uint32_t w[4];
 #pragma unroll
@@ -212,8 +222,8 @@ __device__ __forceinline__ void write_global(T* at, bool ok, const Num<V> (&n)[k
                 w[i] = *reinterpret_cast<const uint32_t*>(&h);
             }
         }
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %5, 0;\n\t@p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n\t}"
-                     ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(p) : "memory");
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %5, %6;\n\t@p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n\t}"
+                     ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(column), "r"(columns) : "memory");
     }
 }
 

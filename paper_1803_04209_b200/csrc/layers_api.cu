@@ -77,7 +77,7 @@ void launch_dropout(DropoutArgs& a, int sms, cudaStream_t s) {
 
 // ---- norms -----------------------------------------------------------------------------------------------------------
 bool bad_layer(const cutoff_norm_layer* l) {
-    return !l || l->rows < 0 || l->rows > INT32_MAX || l->cols < 1 || !known_type(l->type) || !l->x || l->x_ld < l->cols || bad_matrix(l->h, l->h_ld, l->cols) ||
+    return !l || l->rows < 0 || l->rows > kMostRows || l->cols < 1 || !known_type(l->type) || !l->x || l->x_ld < l->cols || bad_matrix(l->h, l->h_ld, l->cols) ||
            bad_matrix(l->gate, l->gate_ld, l->cols) || (l->gate && (l->gate_rows < 1 || !l->h)) || l->gate_kind < CUTOFF_GATE_LINEAR ||
            l->gate_kind > CUTOFF_GATE_SILU || l->post < CUTOFF_NORM_NONE || l->post > CUTOFF_NORM_LAYER || l->pre < CUTOFF_NORM_NONE ||
            l->pre > CUTOFF_NORM_LAYER || !(l->eps > 0.f) || !std::isfinite(l->eps) || (!l->h && (l->scale || l->post_weight || l->post_bias));
@@ -234,7 +234,7 @@ int cutoff_residual_norm(int device, const cutoff_norm_layer* layer, void* resid
 }
 
 int64_t cutoff_residual_norm_grad_workspace_bytes(int64_t rows, int32_t cols) {
-    if (rows < 0 || rows > INT32_MAX || cols < 1 || cols > kMostCols) return CUTOFF_ERR_BAD_ARG;
+    if (rows < 0 || rows > kMostRows || cols < 1 || cols > kMostCols) return CUTOFF_ERR_BAD_ARG;
     // the largest of what the ways to lay out the teams take
     int64_t most = 0;
     for (const int way : {0, 1, 2}) {
@@ -278,7 +278,7 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
                        rows_aligned(grads->gate, grads->gate_ld, size, 16);
     const bool sums = grads->scale || grads->post_weight || grads->post_bias || grads->pre_weight || grads->pre_bias;
     q.column_blocks = sums ? ceil_div(layer->cols, kFinishColumns) : 0;
-    const int gate_blocks = groups && grads->gate && layer->rows > 0 ? plan.teams < 2 * sms ? plan.teams : 2 * sms : 0;
+    const int gate_blocks = groups && grads->gate && layer->rows > 0 ? plan.teams * ceil_div(layer->cols, kFinishColumns * kFinishSlices) : 0;
     bool ok = false;
     with_type(layer->type, [&](auto t) { ok = run_norm_grad<decltype(t)>(q, plan, packs, bias, groups, q.column_blocks + gate_blocks, s); });
     if (!ok) return CUTOFF_ERR_CUDA;

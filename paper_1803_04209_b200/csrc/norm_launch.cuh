@@ -112,9 +112,8 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
     if (plan.lanes == 4) run(eight, integral_constant<int, 4>{});
     else if (plan.lanes == 16) run(eight, integral_constant<int, 16>{});
     else if (plan.lanes == 32 && plan.values == 8) run(eight, integral_constant<int, 32>{});
-    else if (plan.lanes == 32) {
-        if constexpr (!BIAS && !GROUPS) run(sixteen, integral_constant<int, 32>{});       // otherwise a CTA has the row
-    } else if (plan.values == 8) {
+    else if (plan.lanes == 32) run(sixteen, integral_constant<int, 32>{});
+    else if (plan.values == 8) {
         if constexpr (BIAS || GROUPS || sizeof(T) == 4) run(eight, integral_constant<int, 0>{});
     } else run(sixteen, integral_constant<int, 0>{});
     return ok;

@@ -19,6 +19,8 @@ namespace layers {
 enum : int { kNormNone = 0, kNormRms = 1, kNormLayer = 2 };
 enum : int { kGateLinear = 0, kGateSigmoid = 1, kGateSilu = 2 };
 
+constexpr int kMostRows = 1 << 30;
+
 struct NormArgs {
     const void *x, *h, *gate;                     // h: null = no block before (r = x); gate: null = 1
     const float *scale, *post_w, *post_b, *pre_w, *pre_b;
@@ -174,7 +176,7 @@ __device__ __forceinline__ void write_floats(float* p, const Num<V> (&n)[kNums<V
     }
 }
 
-constexpr int kNormWarpThreads = 256;            // CTA of warp teams
+constexpr int kNormWarpThreads = 128;            // CTA of warp teams
 
 // Most threads of a CTA: a CTA team has up to 8192 / (K * V) threads.
 template <int SIZE, int V, int K>
@@ -200,10 +202,12 @@ constexpr int kTeamsHere = SIZE ? kNormWarpThreads / (SIZE ? SIZE : 1) : 1;
     __syncthreads();
 
 // A pack of an operand; single values beyond the row, or of a row that the team does not have, are zeros (packs beyond the row are zeros in shared memory).
+// columns: of the row, or none.
 template <typename T, int V, int SIZE, int K>
-__device__ __forceinline__ void take(uint32_t row_at, const Columns<SIZE, V, K>& col, int k, bool mine, Num<V> (&f)[kNums<V>]) {
-    read_shared<T, V>(row_at + col(k) * static_cast<int>(sizeof(T)), (V > 1 || col.has(k)) && (SIZE == 0 || mine), f);
+__device__ __forceinline__ void take(uint32_t row_at, const Columns<SIZE, V, K>& col, int k, int columns, Num<V> (&f)[kNums<V>]) {
+    read_shared<T, V, V == 1 || SIZE != 0>(row_at + col(k) * static_cast<int>(sizeof(T)), col(k), columns, f);
 }
+
 // The gate of a group of rows, as a team that goes through the rows in their order keeps it.  Zeros beyond the row (where an infinite gate would turn
 // zeros into NaN).
 template <typename T, int V, int K>
@@ -248,7 +252,7 @@ struct TeamRows {
     int first, last, step;
     __device__ __forceinline__ TeamRows(int t, int teams, int rows)
         : first(GROUPS ? first_row_of(t, teams, rows) : t), last(GROUPS ? first_row_of(t + 1, teams, rows) : rows), step(GROUPS ? 1 : teams) {}
-    __device__ __forceinline__ int64_t operator()(int turn) const { return first + static_cast<int64_t>(turn) * step; }
+    __device__ __forceinline__ int operator()(int turn) const { return first + turn * step; }     // rows are few enough (kMostRows) for the turns behind the last
     __device__ __forceinline__ bool has(int turn) const { return (*this)(turn) < last; }
 };
 
@@ -287,12 +291,13 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
         }
     }
     for (int turn = 0; turn < turns; ++turn) {
-        const int64_t row = rows(turn);
+        const int row = rows(turn);
         const int stage = operands.stages == 2 ? turn & 1 : 0;
         const bool mine = rows.has(turn);         // a warp's teams may have a row more or less
+        const int columns = !SIZE || mine ? a.cols : 0;
         if (!SIZE && !mine) break;
         if constexpr (GROUPS)
-            if (mine) group_gate.turn_to(static_cast<int>(row) / a.gate_rows, a.gate, a.gate_ld, col);
+            if (mine) group_gate.turn_to(row / a.gate_rows, a.gate, a.gate_ld, col);
         failed = failed || (mine && !pipe.wait(turn));
         const float eps = failed ? __int_as_float(0x7fc00000) : a.eps;         // what did not arrive gives NaN
         const uint32_t x_at = pipe.template row_at<V>(stage, 0, row);
@@ -300,19 +305,19 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
         if (a.h) {
             const uint32_t h_at = pipe.template row_at<V>(stage, at_h, row);
 #pragma unroll
-            for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, mine, r[k]);
+            for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, columns, r[k]);
             normalise<LAYER, SIZE, V, K>(r, team, col, a.post, eps, a.inv_cols);
             T* const r_row = static_cast<T*>(a.r) + row * a.r_ld;
             const uint32_t gate_at = !GROUPS && a.gate ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 N t[M], x[M];
-                take<T, V>(x_at, col, k, mine, x);
+                take<T, V>(x_at, col, k, columns, x);
 #pragma unroll
                 for (int i = 0; i < M; ++i) r[k][i] = BIAS ? fma(r[k][i], post_w[k][i], post_b[BIAS ? k : 0][i]) : mul(r[k][i], post_w[k][i]);
                 if (a.gate) {
                     if constexpr (GROUPS) group_gate.get(GROUPS ? k : 0, t);
-                    else take<T, V>(gate_at, col, k, mine, t);
+                    else take<T, V>(gate_at, col, k, columns, t);
                     gate_values<false>(t, a.gate_kind, t);
 #pragma unroll
                     for (int i = 0; i < M; ++i) r[k][i] = fma(r[k][i], t[i], x[i]);
@@ -320,11 +325,11 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
 #pragma unroll
                     for (int i = 0; i < M; ++i) r[k][i] = add(r[k][i], x[i]);
                 }
-                if (a.r) write_global<T, V>(r_row + col(k), mine && col.has(k), r[k]);
+                if (a.r) write_global<T, V>(r_row, col(k), columns, r[k]);
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < K; ++k) take<T, V>(x_at, col, k, mine, r[k]);
+            for (int k = 0; k < K; ++k) take<T, V>(x_at, col, k, columns, r[k]);
         }
         // this row's values have been used, by all of the team
         if (turn + operands.stages < turns) {
@@ -340,7 +345,7 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
         if (!a.n_scale) {
             T* const n_row = static_cast<T*>(a.n) + row * a.n_ld;
 #pragma unroll
-            for (int k = 0; k < K; ++k) write_global<T, V>(n_row + col(k), mine && col.has(k), r[k]);
+            for (int k = 0; k < K; ++k) write_global<T, V>(n_row, col(k), columns, r[k]);
             continue;
         }
         uint32_t top = 0;                         // beyond the row everything is zero, the parameters too
@@ -378,11 +383,14 @@ struct NormGradArgs {
     int param_bytes;                              // offset in shared memory of the parameters: scale * post_w, pre_w, with BIAS scale * post_b
 };
 constexpr int kGradThreads = 512;                 // most threads of a CTA: 128 registers each
+// CTAs of warp teams per SM: 128 registers for each thread, 168 with 16 values and many sums.
+template <int VALUES, bool MORE>
+constexpr int kGradWarpCtas = VALUES > 8 && MORE ? 3 : 4;
 
 // GROUPS: a gate for each group of rows, whose gradient is a sum over them.  BIAS: either norm has one, so that the plain sums are needed.
 // SHARED: the parameters are in shared memory (there is no room for them beside one row of five fp32 operands of 8192 values).
 template <typename T, int V, int K, int SIZE, bool BIAS, bool GROUPS, bool LAYER, bool SHARED>
-__global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ? 2 : 1) k_residual_norm_grad(NormGradArgs g, const __grid_constant__ RowOperands operands) {
+__global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ? kGradWarpCtas<V * K, BIAS || GROUPS> : 1) k_residual_norm_grad(NormGradArgs g, const __grid_constant__ RowOperands operands) {
     using N = Num<V>;
     constexpr int M = kNums<V>;
     const NormArgs& a = g.f;
@@ -445,26 +453,27 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
     }
     __syncthreads();
     for (int turn = 0; turn < turns; ++turn) {
-        const int64_t row = rows(turn);
+        const int row = rows(turn);
         const int stage = operands.stages == 2 ? turn & 1 : 0;
         const bool mine = rows.has(turn);
+        const int columns = !SIZE || mine ? a.cols : 0;
         if (!SIZE && !mine) break;
         failed = failed || (mine && !pipe.wait(turn));
         const float eps = failed ? __int_as_float(0x7fc00000) : a.eps;         // what did not arrive gives NaN
-        const int group = GROUPS && mine ? static_cast<int>(row) / a.gate_rows : 0;
+        const int group = GROUPS && mine ? row / a.gate_rows : 0;
         if constexpr (GROUPS)
             if (mine) group_gate.turn_to(group, a.gate, a.gate_ld, col);
         const uint32_t gate_at = has_gate_rows ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
         const auto gate_of = [&](int k, N (&u)[M]) {
             if constexpr (GROUPS) group_gate.get(GROUPS ? k : 0, u);
-            else take<T, V>(gate_at, col, k, mine, u);
+            else take<T, V>(gate_at, col, k, columns, u);
         };
         N hat[K][M], d[K][M];                     // d: the whole gradient at r
         float h_inv = 1.f;
         if (a.h) {
             const uint32_t h_at = pipe.template row_at<V>(stage, at_h, row);
 #pragma unroll
-            for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, mine, hat[k]);
+            for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, columns, hat[k]);
             h_inv = normalise<LAYER, SIZE, V, K>(hat, team, col, a.post, eps, a.inv_cols);
         }
         const uint32_t d_r_at = g.d_r ? pipe.template row_at<V>(stage, at_r, row) : 0u;
@@ -473,7 +482,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
             const uint32_t x_at = pipe.template row_at<V>(stage, 0, row), d_n_at = pipe.template row_at<V>(stage, at_n, row);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                take<T, V>(x_at, col, k, mine, r[k]);
+                take<T, V>(x_at, col, k, columns, r[k]);
                 if (!a.h) continue;
                 N w[M], u[M];
                 param_of(0, k, w);
@@ -502,7 +511,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
             const float r_inv = normalise<LAYER, SIZE, V, K>(r, team, col, a.pre, eps, a.inv_cols);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                take<T, V>(d_n_at, col, k, mine, d[k]);
+                take<T, V>(d_n_at, col, k, columns, d[k]);
 #pragma unroll
                 for (int i = 0; i < M; ++i) {
                     n_hat[k][i] = fma(d[k][i], r[k][i], n_hat[k][i]);
@@ -518,19 +527,19 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     N dr[M];
-                    take<T, V>(d_r_at, col, k, mine, dr);
+                    take<T, V>(d_r_at, col, k, columns, dr);
 #pragma unroll
                     for (int i = 0; i < M; ++i) d[k][i] = add(d[k][i], dr[i]);
                 }
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < K; ++k) take<T, V>(d_r_at, col, k, mine, d[k]);
+            for (int k = 0; k < K; ++k) take<T, V>(d_r_at, col, k, columns, d[k]);
         }
         if (g.d_x) {
             T* const out = static_cast<T*>(g.d_x) + row * g.d_x_ld;
 #pragma unroll
-            for (int k = 0; k < K; ++k) write_global<T, V>(out + col(k), mine && col.has(k), d[k]);
+            for (int k = 0; k < K; ++k) write_global<T, V>(out, col(k), columns, d[k]);
         }
         if (a.h) {
 #pragma unroll
@@ -557,7 +566,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                         } else {
 #pragma unroll
                             for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], mul(d[k][i], p[i]));
-                            write_global<T, V>(static_cast<T*>(g.d_gate) + row * g.d_gate_ld + col(k), mine && col.has(k), slope);
+                            write_global<T, V>(static_cast<T*>(g.d_gate) + row * g.d_gate_ld, col(k), columns, slope);
                         }
                     } else {
                         gate_values<false>(u, a.gate_kind, slope);
@@ -583,11 +592,11 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                 through_norm<LAYER, SIZE, V, K>(d, hat, h_inv, team, a.post, a.inv_cols);
                 T* const out = static_cast<T*>(g.d_h) + row * g.d_h_ld;
 #pragma unroll
-                for (int k = 0; k < K; ++k) write_global<T, V>(out + col(k), mine && col.has(k), d[k]);
+                for (int k = 0; k < K; ++k) write_global<T, V>(out, col(k), columns, d[k]);
             }
             if constexpr (GROUPS) {
                 // the last row of a group, or of this team: the sum is the gradient, or this team's part of it
-                if (mine && (row + 1 == rows.last || static_cast<int>(row + 1) / a.gate_rows != group)) {
+                if (mine && (row + 1 == rows.last || (row + 1) / a.gate_rows != group)) {
                     const int64_t start = static_cast<int64_t>(group) * a.gate_rows, end = min(start + a.gate_rows, static_cast<int64_t>(a.rows));
                     const bool whole = start >= rows.first && end <= rows.last;
                     float* const part = g.gate_sums + (2 * static_cast<int64_t>(t) + (start < rows.first ? 0 : 1)) * a.cols;
@@ -600,7 +609,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                                 gate_values<true>(u, a.gate_kind, slope);
 #pragma unroll
                                 for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], gate_sum[k][i]);
-                                if (g.d_gate) write_global<T, V>(static_cast<T*>(g.d_gate) + group * g.d_gate_ld + col(k), true, slope);
+                                if (g.d_gate) write_global<T, V>(static_cast<T*>(g.d_gate) + group * g.d_gate_ld, col(k), a.cols, slope);
                             } else {
                                 write_floats<V>(part + col(k), gate_sum[k], false);
                             }
@@ -658,23 +667,23 @@ __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_fi
     const NormArgs& a = q.g.f;
     dependency_wait();
     if (static_cast<int>(blockIdx.x) >= q.column_blocks) {
-        // team t begins a group that it does not end: the parts of that group, in the teams' order
-        for (int t = static_cast<int>(blockIdx.x) - q.column_blocks; t < q.g.teams; t += static_cast<int>(gridDim.x) - q.column_blocks) {
-            const int first = first_row_of(t, q.g.teams, a.rows), last = first_row_of(t + 1, q.g.teams, a.rows);
-            if (first == last) continue;
-            const int64_t group = (last - 1) / a.gate_rows, start = group * a.gate_rows, end = min(start + a.gate_rows, static_cast<int64_t>(a.rows));
-            if (start < first || end <= last) continue;
-            int stop = t + 1;                     // the first team that begins behind the group; teams without rows are all at the end
-            while (stop < q.g.teams && first_row_of(stop, q.g.teams, a.rows) < end) ++stop;
-            for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
-                float s = q.g.gate_sums[(2 * static_cast<int64_t>(t) + 1) * a.cols + c];
+        // team t begins a group that it does not end: the parts of that group, in the teams' order, for 512 columns per block
+        const int chunks = ceil_div(a.cols, kFinishColumns * kFinishSlices), at = static_cast<int>(blockIdx.x) - q.column_blocks;
+        const int t = at / chunks, c = at % chunks * kFinishColumns * kFinishSlices + threadIdx.x;
+        const int each = a.rows / q.g.teams, more = a.rows % q.g.teams;
+        const auto first_of = [&](int v) { return each * v + min(v, more); };
+        const int first = first_of(t), last = first_of(t + 1);
+        if (first == last || c >= a.cols) return;
+        const int64_t group = (last - 1) / a.gate_rows, start = group * a.gate_rows, end = min(start + a.gate_rows, static_cast<int64_t>(a.rows));
+        if (start < first || end <= last) return;
+        int stop = t + 1;                         // the first team that begins behind the group; teams without rows are all at the end
+        while (stop < q.g.teams && first_of(stop) < end) ++stop;
+        float s = q.g.gate_sums[(2 * static_cast<int64_t>(t) + 1) * a.cols + c];
 #pragma unroll 8                                   // loads that wait for nothing
-                for (int v = t + 1; v < stop; ++v) s += q.g.gate_sums[2 * static_cast<int64_t>(v) * a.cols + c];
-                F1 u[1] = {F1{to_float(static_cast<const T*>(a.gate)[group * a.gate_ld + c])}}, slope[1];
-                gate_values<true>(u, a.gate_kind, slope);
-                from_float(static_cast<T*>(q.g.d_gate)[group * q.g.d_gate_ld + c], s * slope[0].v);
-            }
-        }
+        for (int v = t + 1; v < stop; ++v) s += q.g.gate_sums[2 * static_cast<int64_t>(v) * a.cols + c];
+        F1 u[1] = {F1{to_float(static_cast<const T*>(a.gate)[group * a.gate_ld + c])}}, slope[1];
+        gate_values<true>(u, a.gate_kind, slope);
+        from_float(static_cast<T*>(q.g.d_gate)[group * q.g.d_gate_ld + c], s * slope[0].v);
         return;
     }
     const int x = threadIdx.x % kFinishColumns, slice = threadIdx.x / kFinishColumns, c = blockIdx.x * kFinishColumns + x;
@@ -720,10 +729,11 @@ struct GradPlan {
 constexpr int kMostSms = 160, kMostTeamRows = 1024;          // a team adds at most this many rows in a row
 inline GradPlan grad_plan(int rows, int cols, int type_size, bool many_sums, int sms) {
     GradPlan p;
-    p.lanes = cols <= 32 ? 4 : cols <= 128 ? 16 : cols <= 256 || (cols <= 512 && !many_sums) ? 32 : 0;
+    p.lanes = cols <= 32 ? 4 : cols <= 128 ? 16 : cols <= 512 ? 32 : 0;
     p.values = p.lanes ? (cols <= 256 ? 8 : 16) : (many_sums || type_size == 4) && cols <= 8 * kGradThreads ? 8 : 16;
     p.threads = p.lanes ? kNormWarpThreads : ceil_div(ceil_div(cols, p.values), 32) * 32;
-    p.per_sm = kGradThreads / p.threads;                      // by the registers; shared memory may allow fewer
+    // by the registers; shared memory may allow fewer
+    p.per_sm = p.lanes ? (p.values > 8 && many_sums ? kGradWarpCtas<16, true> : kGradWarpCtas<8, false>) : kGradThreads / p.threads;
     const int per_cta = p.lanes ? p.threads / p.lanes : 1;
     const int few = ceil_div(rows, per_cta), many = ceil_div(few, kMostTeamRows), resident = (sms < kMostSms ? sms : kMostSms) * p.per_sm;
     p.ctas = resident < many ? many : resident;
