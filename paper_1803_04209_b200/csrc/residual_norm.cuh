@@ -40,27 +40,29 @@ __device__ __forceinline__ float logistic(float g) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
     return s;
 }
-// g becomes act(g), and with SLOPE slope its derivative; the kind is the same for a whole call, so that one branch serves a pack.
-template <bool SLOPE, typename N, int M>
-__device__ __forceinline__ void gate_values(N (&g)[M], int kind, N (&slope)[M]) {
-    if (kind == kGateLinear) {
-        if constexpr (SLOPE)
+// g becomes act(g), and with SLOPE slope its derivative.
+template <int KIND, bool SLOPE, typename N, int M>
+__device__ __forceinline__ void gate_values(N (&g)[M], N (&slope)[M]) {
 #pragma unroll
-            for (int i = 0; i < M; ++i) slope[i] = splat<N>(1.f);
-    } else if (kind == kGateSigmoid) {
-#pragma unroll
-        for (int i = 0; i < M; ++i) {
+    for (int i = 0; i < M; ++i) {
+        if constexpr (KIND == kGateLinear) {
+            if constexpr (SLOPE) slope[i] = splat<N>(1.f);
+        } else if constexpr (KIND == kGateSigmoid) {
             g[i] = each(g[i], logistic);
             if constexpr (SLOPE) slope[i] = fma(mul(g[i], splat<N>(-1.f)), g[i], g[i]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < M; ++i) {
+        } else {
             const N t = each(g[i], logistic);
             g[i] = mul(g[i], t);
             if constexpr (SLOPE) slope[i] = fma(g[i], fma(t, splat<N>(-1.f), splat<N>(1.f)), t);
         }
     }
+}
+// f(kind as a constant): the kind is the same for a whole call, and one branch serves a thread's whole row.
+template <typename F>
+__device__ __forceinline__ void with_gate(int kind, F f) {
+    if (kind == kGateLinear) f(std::integral_constant<int, kGateLinear>{});
+    else if (kind == kGateSigmoid) f(std::integral_constant<int, kGateSigmoid>{});
+    else f(std::integral_constant<int, kGateSilu>{});
 }
 
 // The team's columns: K packs of V values per thread.
@@ -308,24 +310,36 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
             for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, columns, r[k]);
             normalise<LAYER, SIZE, V, K>(r, team, col, a.post, eps, a.inv_cols);
             T* const r_row = static_cast<T*>(a.r) + row * a.r_ld;
+            const int r_columns = a.r ? columns : 0;
             const uint32_t gate_at = !GROUPS && a.gate ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                N t[M], x[M];
-                take<T, V>(x_at, col, k, columns, x);
+            for (int k = 0; k < K; ++k)
 #pragma unroll
                 for (int i = 0; i < M; ++i) r[k][i] = BIAS ? fma(r[k][i], post_w[k][i], post_b[BIAS ? k : 0][i]) : mul(r[k][i], post_w[k][i]);
-                if (a.gate) {
-                    if constexpr (GROUPS) group_gate.get(GROUPS ? k : 0, t);
-                    else take<T, V>(gate_at, col, k, columns, t);
-                    gate_values<false>(t, a.gate_kind, t);
+            const auto add_x = [&](int k, const N (&t)[M]) {              // r = x + t r, and out it goes
+                N x[M];
+                take<T, V>(x_at, col, k, columns, x);
 #pragma unroll
-                    for (int i = 0; i < M; ++i) r[k][i] = fma(r[k][i], t[i], x[i]);
-                } else {
+                for (int i = 0; i < M; ++i) r[k][i] = fma(r[k][i], t[i], x[i]);
+                write_global<T, V>(r_row, col(k), r_columns, r[k]);
+            };
+            if (a.gate) {
+                with_gate(a.gate_kind, [&](auto kind) {
 #pragma unroll
-                    for (int i = 0; i < M; ++i) r[k][i] = add(r[k][i], x[i]);
-                }
-                if (a.r) write_global<T, V>(r_row, col(k), columns, r[k]);
+                    for (int k = 0; k < K; ++k) {
+                        N t[M];
+                        if constexpr (GROUPS) group_gate.get(GROUPS ? k : 0, t);
+                        else take<T, V>(gate_at, col, k, columns, t);
+                        gate_values<decltype(kind)::value, false>(t, t);
+                        add_x(k, t);
+                    }
+                });
+            } else {
+                N one[M];
+#pragma unroll
+                for (int i = 0; i < M; ++i) one[i] = splat<N>(1.f);
+#pragma unroll
+                for (int k = 0; k < K; ++k) add_x(k, one);
             }
         } else {
 #pragma unroll
@@ -480,28 +494,45 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
         if (g.d_n) {
             N r[K][M];
             const uint32_t x_at = pipe.template row_at<V>(stage, 0, row), d_n_at = pipe.template row_at<V>(stage, at_n, row);
+            if (a.h) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                take<T, V>(x_at, col, k, columns, r[k]);
-                if (!a.h) continue;
-                N w[M], u[M];
-                param_of(0, k, w);
+                for (int k = 0; k < K; ++k) {
+                    N w[M];
+                    param_of(0, k, w);
 #pragma unroll
-                for (int i = 0; i < M; ++i) w[i] = mul(w[i], hat[k][i]);
-                if constexpr (BIAS) {
-                    param_of(2, k, u);
+                    for (int i = 0; i < M; ++i) r[k][i] = mul(w[i], hat[k][i]);
+                    if constexpr (BIAS) {
+                        param_of(2, k, w);
 #pragma unroll
-                    for (int i = 0; i < M; ++i) w[i] = add(w[i], u[i]);
+                        for (int i = 0; i < M; ++i) r[k][i] = add(r[k][i], w[i]);
+                    }
                 }
+                const auto add_x = [&](int k, const N (&t)[M]) {          // r = x + t r
+                    N x[M];
+                    take<T, V>(x_at, col, k, columns, x);
+#pragma unroll
+                    for (int i = 0; i < M; ++i) r[k][i] = fma(r[k][i], t[i], x[i]);
+                };
                 if (a.gate) {
-                    gate_of(k, u);
-                    gate_values<false>(u, a.gate_kind, u);
+                    with_gate(a.gate_kind, [&](auto kind) {
 #pragma unroll
-                    for (int i = 0; i < M; ++i) r[k][i] = fma(w[i], u[i], r[k][i]);
+                        for (int k = 0; k < K; ++k) {
+                            N t[M];
+                            gate_of(k, t);
+                            gate_values<decltype(kind)::value, false>(t, t);
+                            add_x(k, t);
+                        }
+                    });
                 } else {
+                    N one[M];
 #pragma unroll
-                    for (int i = 0; i < M; ++i) r[k][i] = add(r[k][i], w[i]);
+                    for (int i = 0; i < M; ++i) one[i] = splat<N>(1.f);
+#pragma unroll
+                    for (int k = 0; k < K; ++k) add_x(k, one);
                 }
+            } else {
+#pragma unroll
+                for (int k = 0; k < K; ++k) take<T, V>(x_at, col, k, columns, r[k]);
             }
             if (SIZE != 0 && !mine)               // a bias would be left of a row that there is not
 #pragma unroll
@@ -536,22 +567,32 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
 #pragma unroll
             for (int k = 0; k < K; ++k) take<T, V>(d_r_at, col, k, columns, d[k]);
         }
-        if (g.d_x) {
+        {
             T* const out = static_cast<T*>(g.d_x) + row * g.d_x_ld;
+            const int x_columns = g.d_x ? columns : 0;
 #pragma unroll
-            for (int k = 0; k < K; ++k) write_global<T, V>(out, col(k), columns, d[k]);
+            for (int k = 0; k < K; ++k) write_global<T, V>(out, col(k), x_columns, d[k]);
         }
         if (a.h) {
+            // e = d act(gate) and the gradient at the branch's hat; w is scale * post_w, zero beyond the row, whatever a layer norm's gradient left in d
+            const auto at_hat = [&](int k, const N (&w)[M]) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                N w[M];                           // scale * post_w; beyond the row it is zero, whatever a layer norm's gradient left in d
-                param_of(0, k, w);
-                if (a.gate) {
-                    N u[M], slope[M];
-                    gate_of(k, u);
-                    if (GROUPS || g.d_gate) {
-                        gate_values<!GROUPS>(u, a.gate_kind, slope);
-                        N p[M];
+                for (int i = 0; i < M; ++i) {
+                    e_hat[k][i] = fma(d[k][i], hat[k][i], e_hat[k][i]);
+                    if constexpr (BIAS) e_sum[k][i] = add(e_sum[k][i], d[k][i]);
+                    d[k][i] = mul(d[k][i], w[i]);
+                }
+            };
+            if (a.gate) {
+                T* const gate_row = static_cast<T*>(g.d_gate) + row * g.d_gate_ld;
+                const int gate_columns = g.d_gate ? columns : 0;
+                with_gate(a.gate_kind, [&](auto kind) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        N w[M], u[M], slope[M], p[M];
+                        param_of(0, k, w);
+                        gate_of(k, u);
+                        gate_values<decltype(kind)::value, !GROUPS>(u, slope);
 #pragma unroll
                         for (int i = 0; i < M; ++i) p[i] = mul(hat[k][i], w[i]);
                         if constexpr (BIAS) {
@@ -566,19 +607,19 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                         } else {
 #pragma unroll
                             for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], mul(d[k][i], p[i]));
-                            write_global<T, V>(static_cast<T*>(g.d_gate) + row * g.d_gate_ld, col(k), columns, slope);
+                            write_global<T, V>(gate_row, col(k), gate_columns, slope);
                         }
-                    } else {
-                        gate_values<false>(u, a.gate_kind, slope);
+#pragma unroll
+                        for (int i = 0; i < M; ++i) d[k][i] = mul(d[k][i], u[i]);
+                        at_hat(k, w);
                     }
+                });
+            } else {
 #pragma unroll
-                    for (int i = 0; i < M; ++i) d[k][i] = mul(d[k][i], u[i]);
-                }
-#pragma unroll
-                for (int i = 0; i < M; ++i) {
-                    e_hat[k][i] = fma(d[k][i], hat[k][i], e_hat[k][i]);
-                    if constexpr (BIAS) e_sum[k][i] = add(e_sum[k][i], d[k][i]);
-                    d[k][i] = mul(d[k][i], w[i]);
+                for (int k = 0; k < K; ++k) {
+                    N w[M];
+                    param_of(0, k, w);
+                    at_hat(k, w);
                 }
             }
         }
@@ -606,7 +647,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                             if (whole) {
                                 N u[M], slope[M];
                                 gate_of(k, u);
-                                gate_values<true>(u, a.gate_kind, slope);
+                                with_gate(a.gate_kind, [&](auto kind) { gate_values<decltype(kind)::value, true>(u, slope); });
 #pragma unroll
                                 for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], gate_sum[k][i]);
                                 if (g.d_gate) write_global<T, V>(static_cast<T*>(g.d_gate) + group * g.d_gate_ld, col(k), a.cols, slope);
@@ -682,7 +723,7 @@ __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_fi
 #pragma unroll 8                                   // loads that wait for nothing
         for (int v = t + 1; v < stop; ++v) s += q.g.gate_sums[2 * static_cast<int64_t>(v) * a.cols + c];
         F1 u[1] = {F1{to_float(static_cast<const T*>(a.gate)[group * a.gate_ld + c])}}, slope[1];
-        gate_values<true>(u, a.gate_kind, slope);
+        with_gate(a.gate_kind, [&](auto kind) { gate_values<decltype(kind)::value, true>(u, slope); });
         from_float(static_cast<T*>(q.g.d_gate)[group * q.g.d_gate_ld + c], s * slope[0].v);
         return;
     }
