@@ -439,7 +439,7 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
 /* Products in 8-bit integers with a scale for each row of either operand (token and output channel).
  *
  * cutoff_quantize_rows: scale[i] = max_j |x[i][j]| / 127, q[i][j] = rint(x[i][j] * (127 / max)) in single precision (ties to even), -127 .. 127.  A row
- * of magnitudes below 2^-100 gives zeros; a row with a NaN or an infinity gives a scale that is NaN or infinite, and so NaN in its products.
+ * of magnitudes below 2^-100 gives zeros; a row with a NaN or an infinity gives a scale that is NaN or infinite and integers of no meaning, and so NaN or infinity in its products.
  *
  * cutoff_quantized_product: y[i][j] = (sum_k a[i][k] b[j][k]) * a_scale[i] * b_scale[j] + bias[j], y m x n of `type`; the sum is exact.  a: m x k,
  * b: n x k int8; both start on 16 bytes and their leading dimensions are multiples of 16 (BAD_ARG otherwise); whatever lies behind a row's k values

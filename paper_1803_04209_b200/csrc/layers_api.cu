@@ -297,8 +297,20 @@ int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, c
     with_type(type, [&](auto t) {
         using T = decltype(t);
         const bool packs = cols % kPack<T> == 0 && rows_aligned(x, x_ld, size, 16) && rows_aligned(q, q_ld, 1, kPack<T>);
-        launch_dependent(packs ? k_quantize_rows<T, kPack<T>> : k_quantize_rows<T, 1>, dim3(static_cast<unsigned>(rows)), dim3(kQuantizeThreads), 0,
-                         static_cast<cudaStream_t>(stream), a);
+        const auto run = [&](auto v) {
+            constexpr int V = decltype(v)::value;
+            const cudaStream_t s = static_cast<cudaStream_t>(stream);
+            // rows that a warp holds in registers; otherwise a CTA whose threads hold four packs each, or with few rows (their latency is all there is) one
+            if (cols <= 32 * V * kQuantizeKeep && rows > sm_count(device)) {
+                launch_dependent(k_quantize_rows<T, V, 32>, dim3(static_cast<unsigned>(ceil_div64(rows, kQuantizeWarps))), dim3(kQuantizeWarps * 32), 0, s, a);
+                return;
+            }
+            int threads = ceil_div(ceil_div(cols, rows > 2 * sm_count(device) ? V * kQuantizeKeep : V), 32) * 32;
+            threads = threads > 512 ? 512 : threads;
+            launch_dependent(k_quantize_rows<T, V, 0>, dim3(static_cast<unsigned>(rows)), dim3(threads), 0, s, a);
+        };
+        if (packs) run(std::integral_constant<int, kPack<T>>{});
+        else run(std::integral_constant<int, 1>{});
     });
     return status();
 }
