@@ -358,8 +358,10 @@ int cutoff_adam_step(int device, int64_t n, float* params, const float* grads, f
  * Matrices are row-major with a leading dimension (the distance between rows, in values, >= the row's length); what lies between a row's
  * end and the next row is neither read as a value nor written.  An output may be the same matrix as an input of the same call (same address, leading
  * dimension and type); other overlaps are undefined.  Values are `type`; parameters and their gradients are fp32.  Arithmetic and sums are fp32; an output
- * is rounded once.  Rows that start on 16 bytes and have whole packs of 16 bytes are the fastest; nothing else depends on alignment except where
- * said.  Zero rows are allowed; addresses are then not used, but NULL still means absent. */
+ * is rounded once.  Addresses are multiples of their values' size, leading dimensions at most 2^38 (BAD_ARG otherwise).  Rows that start on 16 bytes
+ * and have whole packs of 16 bytes are the fastest; nothing else depends on alignment except where said.  Memory is read in units of 16 bytes: the
+ * bytes around a row up to the next multiples of 16 have to be readable, which they are in any allocation of the CUDA runtime.  Zero rows are allowed;
+ * addresses are then not used, but NULL still means absent. */
 enum { CUTOFF_TYPE_FP32 = 0, CUTOFF_TYPE_FP16 = 1, CUTOFF_TYPE_BF16 = 2 };
 enum { CUTOFF_NORM_NONE = 0, CUTOFF_NORM_RMS = 1, CUTOFF_NORM_LAYER = 2 };
 enum { CUTOFF_GATE_LINEAR = 0, CUTOFF_GATE_SIGMOID = 1, CUTOFF_GATE_SILU = 2 };
@@ -372,7 +374,7 @@ enum { CUTOFF_GATE_LINEAR = 0, CUTOFF_GATE_SIGMOID = 1, CUTOFF_GATE_SILU = 2 };
  * residual.  Guide, transition and emission use the streams below 0x400.
  *   x, y      device, rows x cols;  residual  device, rows x cols, or NULL for zeros
  *   p         0 .. 1; with T = 65536 everything is dropped.  A dropped value is not looked at: NaN or infinity there do no harm.
- *   first_row + rows <= 2^32.  Errors: BAD_ARG, CUDA. */
+ *   first_row + rows <= 2^32, cols <= 2^30 (TOO_LARGE otherwise).  Errors: BAD_ARG, TOO_LARGE, CUDA. */
 int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, const void* residual,
                    int64_t residual_ld, void* y, int64_t y_ld, double p, uint64_t seed, uint32_t step, uint32_t noise_stream, int64_t first_row,
                    void* stream);
@@ -382,7 +384,7 @@ int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const v
  * where post and pre are CUTOFF_NORM_*: RMS v / sqrt(mean(v^2) + eps), LAYER (v - mean(v)) / sqrt(var(v) + eps) (population variance), times the weight
  * plus the bias (NULL: ones, zeros), or NONE, which still applies weight and bias.  gate is a row for every gate_rows rows of x (1: one for each
  * row; the last group may be shorter); act is CUTOFF_GATE_*: g, 1 / (1 + exp(-g)), g / (1 + exp(-g)).  NULL: gate 1, scale 1.  With h NULL
- * there is no block: r = x (scale, gate, post_weight and post_bias must be NULL).  cols <= 8192 (TOO_LARGE otherwise), eps > 0.
+ * there is no block: r = x (scale, gate, post_weight and post_bias must be NULL).  rows <= 2^30, cols <= 8192 (TOO_LARGE otherwise), eps > 0.
  *
  * cutoff_residual_norm: residual (rows x cols, receives r; NULL = not wanted; must be NULL without h) and norm (receives n; NULL = not wanted).
  * With norm_scale (rows floats) n is not stored as `type` but as 8-bit integers as cutoff_quantize_rows makes them of the unrounded n, norm being
@@ -439,12 +441,15 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
 /* Products in 8-bit integers with a scale for each row of either operand (token and output channel).
  *
  * cutoff_quantize_rows: scale[i] = max_j |x[i][j]| / 127, q[i][j] = rint(x[i][j] * (127 / max)) in single precision (ties to even), -127 .. 127.  A row
- * of magnitudes below 2^-100 gives zeros; a row with a NaN or an infinity gives a scale that is NaN or infinite and integers of no meaning, and so NaN or infinity in its products.
+ * of magnitudes below 2^-100 gives zeros; a row with a NaN or an infinity gives a scale that is NaN or infinite and integers of no
+ * meaning, and so NaN or infinity in its products.
  *
  * cutoff_quantized_product: y[i][j] = (sum_k a[i][k] b[j][k]) * a_scale[i] * b_scale[j] + bias[j], y m x n of `type`; the sum is exact.  a: m x k,
  * b: n x k int8; both start on 16 bytes and their leading dimensions are multiples of 16 (BAD_ARG otherwise); whatever lies behind a row's k values
  * is not used, but up to the next multiple of 16 it has to be readable.  bias: n floats or NULL.
- * k <= CUTOFF_PRODUCT_MAX_K (TOO_LARGE otherwise: the sum could leave 32 bits).  Errors of both: BAD_ARG, TOO_LARGE, CUDA. */
+ * m <= 2^30; k <= CUTOFF_PRODUCT_MAX_K (TOO_LARGE otherwise: the sum could leave 32 bits); n, and cols of cutoff_quantize_rows, <= 2^30 (TOO_LARGE).
+ * The tensor-core kernels' waits are bounded: a tile whose operands do not arrive within seconds (a hung device) is written as NaN, as are a norm's rows.
+ * Errors of both: BAD_ARG, TOO_LARGE, CUDA. */
 #define CUTOFF_PRODUCT_MAX_K 131071
 int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, int8_t* q, int64_t q_ld, float* scale,
                          void* stream);

@@ -48,7 +48,11 @@ bool rows_aligned(const void* p, int64_t ld, int size, int bytes) {
     return p == nullptr || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % bytes == 0);
 }
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-bool bad_matrix(const void* p, int64_t ld, int64_t cols) { return p != nullptr && ld < cols; }
+// A matrix that is there with rows that overlap, rows too far apart for 64-bit offsets and tensor maps, or values off their own alignment.
+constexpr int64_t kMostApart = int64_t{1} << 38;
+bool off(const void* p, int size) { return reinterpret_cast<uintptr_t>(p) % size != 0; }
+bool bad_matrix(const void* p, int64_t ld, int64_t cols, int size) { return p != nullptr && (ld < cols || ld > kMostApart || off(p, size)); }
+constexpr int kMostProductCols = 1 << 30;     // of dropout, quantised rows and a product's outputs: columns and a tile more fit 32 bits
 
 // ---- dropout ---------------------------------------------------------------------------------------------------------
 template <typename T, int V, int LX>
@@ -77,8 +81,11 @@ void launch_dropout(DropoutArgs& a, int sms, cudaStream_t s) {
 
 // ---- norms -----------------------------------------------------------------------------------------------------------
 bool bad_layer(const cutoff_norm_layer* l) {
-    return !l || l->rows < 0 || l->rows > kMostRows || l->cols < 1 || !known_type(l->type) || !l->x || l->x_ld < l->cols || bad_matrix(l->h, l->h_ld, l->cols) ||
-           bad_matrix(l->gate, l->gate_ld, l->cols) || (l->gate && (l->gate_rows < 1 || !l->h)) || l->gate_kind < CUTOFF_GATE_LINEAR ||
+    if (!l || !known_type(l->type)) return true;
+    const int size = type_size(l->type);
+    return l->rows < 0 || l->rows > kMostRows || l->cols < 1 || !l->x || bad_matrix(l->x, l->x_ld, l->cols, size) || bad_matrix(l->h, l->h_ld, l->cols, size) ||
+           bad_matrix(l->gate, l->gate_ld, l->cols, size) || off(l->scale, 4) || off(l->post_weight, 4) || off(l->post_bias, 4) || off(l->pre_weight, 4) ||
+           off(l->pre_bias, 4) || (l->gate && (l->gate_rows < 1 || !l->h)) || l->gate_kind < CUTOFF_GATE_LINEAR ||
            l->gate_kind > CUTOFF_GATE_SILU || l->post < CUTOFF_NORM_NONE || l->post > CUTOFF_NORM_LAYER || l->pre < CUTOFF_NORM_NONE ||
            l->pre > CUTOFF_NORM_LAYER || !(l->eps > 0.f) || !std::isfinite(l->eps) || (!l->h && (l->scale || l->post_weight || l->post_bias));
 }
@@ -188,9 +195,10 @@ extern "C" {
 
 int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, const void* residual, int64_t residual_ld,
                    void* y, int64_t y_ld, double p, uint64_t seed, uint32_t step, uint32_t noise_stream, int64_t first_row, void* stream) {
-    if (device < 0 || !known_type(type) || rows < 0 || cols < 1 || !x || !y || x_ld < cols || y_ld < cols || bad_matrix(residual, residual_ld, cols) ||
-        !(p >= 0.0 && p <= 1.0) || first_row < 0 || rows > (int64_t{1} << 32) || first_row > (int64_t{1} << 32) - rows)
+    if (device < 0 || !known_type(type) || rows < 0 || cols < 1 || !x || !y || bad_matrix(x, x_ld, cols, type_size(type)) ||
+        bad_matrix(y, y_ld, cols, type_size(type)) || bad_matrix(residual, residual_ld, cols, type_size(type)) || !(p >= 0.0 && p <= 1.0) || first_row < 0 || rows > (int64_t{1} << 32) || first_row > (int64_t{1} << 32) - rows)
         return CUTOFF_ERR_BAD_ARG;
+    if (cols > kMostProductCols) return CUTOFF_ERR_TOO_LARGE;
     if (rows == 0) return CUTOFF_OK;
     DeviceGuard guard(device);
     if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
@@ -216,8 +224,8 @@ int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const v
 
 int cutoff_residual_norm(int device, const cutoff_norm_layer* layer, void* residual, int64_t residual_ld, void* norm, int64_t norm_ld, float* norm_scale,
                          void* stream) {
-    if (device < 0 || bad_layer(layer) || bad_matrix(residual, residual_ld, layer->cols) || bad_matrix(norm, norm_ld, layer->cols) ||
-        (!residual && !norm) || (!layer->h && residual) || (norm_scale && !norm))
+    if (device < 0 || bad_layer(layer) || bad_matrix(residual, residual_ld, layer->cols, type_size(layer->type)) ||
+        bad_matrix(norm, norm_ld, layer->cols, norm_scale ? 1 : type_size(layer->type)) || off(norm_scale, 4) || (!residual && !norm) || (!layer->h && residual) || (norm_scale && !norm))
         return CUTOFF_ERR_BAD_ARG;
     if (layer->cols > kMostCols) return CUTOFF_ERR_TOO_LARGE;
     if (layer->rows == 0) return CUTOFF_OK;
@@ -247,9 +255,12 @@ int64_t cutoff_residual_norm_grad_workspace_bytes(int64_t rows, int32_t cols) {
 
 int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const void* d_residual, int64_t d_residual_ld, const void* d_norm,
                               int64_t d_norm_ld, const cutoff_norm_grads* grads, void* workspace, size_t workspace_bytes, void* stream) {
-    if (device < 0 || bad_layer(layer) || !grads || bad_matrix(d_residual, d_residual_ld, layer->cols) || bad_matrix(d_norm, d_norm_ld, layer->cols) ||
-        (!d_residual && !d_norm) || bad_matrix(grads->x, grads->x_ld, layer->cols) || bad_matrix(grads->h, grads->h_ld, layer->cols) ||
-        bad_matrix(grads->gate, grads->gate_ld, layer->cols) || (!layer->h && (grads->h || grads->gate)) || (grads->gate && !layer->gate) || !workspace ||
+    if (device < 0 || bad_layer(layer) || !grads) return CUTOFF_ERR_BAD_ARG;
+    const int size = type_size(layer->type);
+    if (bad_matrix(d_residual, d_residual_ld, layer->cols, size) || bad_matrix(d_norm, d_norm_ld, layer->cols, size) || (!d_residual && !d_norm) ||
+        bad_matrix(grads->x, grads->x_ld, layer->cols, size) || bad_matrix(grads->h, grads->h_ld, layer->cols, size) ||
+        bad_matrix(grads->gate, grads->gate_ld, layer->cols, size) || off(grads->scale, 4) || off(grads->post_weight, 4) || off(grads->post_bias, 4) ||
+        off(grads->pre_weight, 4) || off(grads->pre_bias, 4) || (!layer->h && (grads->h || grads->gate)) || (grads->gate && !layer->gate) || !workspace ||
         (grads->scale && !layer->scale) || (grads->post_weight && !layer->post_weight) || (grads->post_bias && !layer->post_bias) ||
         (grads->pre_weight && !layer->pre_weight) || (grads->pre_bias && !layer->pre_bias))
         return CUTOFF_ERR_BAD_ARG;
@@ -272,7 +283,6 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
     g.teams = plan.teams;
     q.ctas = plan.ctas; q.each = bias ? 4 : 2;
     q.d_scale = grads->scale; q.d_post_w = grads->post_weight; q.d_post_b = grads->post_bias; q.d_pre_w = grads->pre_weight; q.d_pre_b = grads->pre_bias;
-    const int size = type_size(layer->type);
     const bool packs = whole_packs(layer) && rows_aligned(d_residual, d_residual_ld, size, 16) && rows_aligned(d_norm, d_norm_ld, size, 16) &&
                        rows_aligned(grads->x, grads->x_ld, size, 16) && rows_aligned(grads->h, grads->h_ld, size, 16) &&
                        rows_aligned(grads->gate, grads->gate_ld, size, 16);
@@ -287,8 +297,10 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
 
 int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, int8_t* q, int64_t q_ld, float* scale,
                          void* stream) {
-    if (device < 0 || !known_type(type) || rows < 0 || rows > INT32_MAX || cols < 1 || !x || !q || !scale || x_ld < cols || q_ld < cols)
+    if (device < 0 || !known_type(type) || rows < 0 || rows > INT32_MAX || cols < 1 || !x || !q || !scale || bad_matrix(x, x_ld, cols, type_size(type)) ||
+        bad_matrix(q, q_ld, cols, 1) || off(scale, 4))
         return CUTOFF_ERR_BAD_ARG;
+    if (cols > kMostProductCols) return CUTOFF_ERR_TOO_LARGE;
     if (rows == 0) return CUTOFF_OK;
     DeviceGuard guard(device);
     if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
@@ -317,10 +329,10 @@ int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, c
 
 int cutoff_quantized_product(int device, int64_t m, int32_t n, int32_t k, const int8_t* a, int64_t a_ld, const float* a_scale, const int8_t* b,
                              int64_t b_ld, const float* b_scale, const float* bias, int32_t type, void* y, int64_t y_ld, void* stream) {
-    if (device < 0 || m < 0 || m > INT32_MAX || n < 1 || k < 1 || !a || !a_scale || !b || !b_scale || !known_type(type) || !y || a_ld < k || b_ld < k || y_ld < n ||
-        !rows_aligned(a, a_ld, 1, 16) || !rows_aligned(b, b_ld, 1, 16))
+    if (device < 0 || m < 0 || m > kMostRows || n < 1 || k < 1 || !a || !a_scale || !b || !b_scale || !known_type(type) || !y || bad_matrix(a, a_ld, k, 1) ||
+        bad_matrix(b, b_ld, k, 1) || bad_matrix(y, y_ld, n, type_size(type)) || off(a_scale, 4) || off(b_scale, 4) || off(bias, 4) || !rows_aligned(a, a_ld, 1, 16) || !rows_aligned(b, b_ld, 1, 16))
         return CUTOFF_ERR_BAD_ARG;
-    if (k > CUTOFF_PRODUCT_MAX_K) return CUTOFF_ERR_TOO_LARGE;
+    if (k > CUTOFF_PRODUCT_MAX_K || n > kMostProductCols) return CUTOFF_ERR_TOO_LARGE;
     if (m == 0) return CUTOFF_OK;
     DeviceGuard guard(device);
     if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;

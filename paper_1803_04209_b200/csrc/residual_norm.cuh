@@ -97,6 +97,16 @@ __device__ __forceinline__ float sum_of(const Values<V, K>& a) {
     return total(s);
 }
 
+// What did not arrive in time is marked.
+template <int V, int K>
+__device__ __forceinline__ void mark(bool failed, Values<V, K>& v) {
+    if (!failed) return;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < kNums<V>; ++i) v[k][i] = splat<Num<V>>(__int_as_float(0x7fc00000));
+}
+
 // v becomes (v - mean) * inv, inv = 1 / sqrt(mean square + eps), over the row; values outside of the row are 0 and stay so.  Returns inv.
 // LAYER: the kind may be a layer norm; without it no mean is looked for.
 template <bool LAYER, int SIZE, int V, int K>
@@ -301,14 +311,14 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
         if constexpr (GROUPS)
             if (mine) group_gate.turn_to(row / a.gate_rows, a.gate, a.gate_ld, col);
         failed = failed || (mine && !pipe.wait(turn));
-        const float eps = failed ? __int_as_float(0x7fc00000) : a.eps;         // what did not arrive gives NaN
         const uint32_t x_at = pipe.template row_at<V>(stage, 0, row);
         N r[K][M];
         if (a.h) {
             const uint32_t h_at = pipe.template row_at<V>(stage, at_h, row);
 #pragma unroll
             for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, columns, r[k]);
-            normalise<LAYER, SIZE, V, K>(r, team, col, a.post, eps, a.inv_cols);
+            mark<V, K>(failed, r);
+            normalise<LAYER, SIZE, V, K>(r, team, col, a.post, a.eps, a.inv_cols);
             T* const r_row = static_cast<T*>(a.r) + row * a.r_ld;
             const int r_columns = a.r ? columns : 0;
             const uint32_t gate_at = !GROUPS && a.gate ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
@@ -344,6 +354,7 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
         } else {
 #pragma unroll
             for (int k = 0; k < K; ++k) take<T, V>(x_at, col, k, columns, r[k]);
+            mark<V, K>(failed, r);
         }
         // this row's values have been used, by all of the team
         if (turn + operands.stages < turns) {
@@ -351,7 +362,7 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
             if (!failed && rows.has(turn + operands.stages)) pipe.fetch(stage, rows(turn + operands.stages), team);
         }
         if (!a.n) continue;
-        normalise<LAYER, SIZE, V, K>(r, team, col, a.pre, eps, a.inv_cols);
+        normalise<LAYER, SIZE, V, K>(r, team, col, a.pre, a.eps, a.inv_cols);
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -473,7 +484,6 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
         const int columns = !SIZE || mine ? a.cols : 0;
         if (!SIZE && !mine) break;
         failed = failed || (mine && !pipe.wait(turn));
-        const float eps = failed ? __int_as_float(0x7fc00000) : a.eps;         // what did not arrive gives NaN
         const int group = GROUPS && mine ? row / a.gate_rows : 0;
         if constexpr (GROUPS)
             if (mine) group_gate.turn_to(group, a.gate, a.gate_ld, col);
@@ -488,7 +498,8 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
             const uint32_t h_at = pipe.template row_at<V>(stage, at_h, row);
 #pragma unroll
             for (int k = 0; k < K; ++k) take<T, V>(h_at, col, k, columns, hat[k]);
-            h_inv = normalise<LAYER, SIZE, V, K>(hat, team, col, a.post, eps, a.inv_cols);
+            mark<V, K>(failed, hat);
+            h_inv = normalise<LAYER, SIZE, V, K>(hat, team, col, a.post, a.eps, a.inv_cols);
         }
         const uint32_t d_r_at = g.d_r ? pipe.template row_at<V>(stage, at_r, row) : 0u;
         if (g.d_n) {
@@ -539,7 +550,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                 for (int k = 0; k < K; ++k)
 #pragma unroll
                     for (int i = 0; i < M; ++i) r[k][i] = splat<N>(0.f);
-            const float r_inv = normalise<LAYER, SIZE, V, K>(r, team, col, a.pre, eps, a.inv_cols);
+            const float r_inv = normalise<LAYER, SIZE, V, K>(r, team, col, a.pre, a.eps, a.inv_cols);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 take<T, V>(d_n_at, col, k, columns, d[k]);
@@ -567,6 +578,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
 #pragma unroll
             for (int k = 0; k < K; ++k) take<T, V>(d_r_at, col, k, columns, d[k]);
         }
+        mark<V, K>(failed, d);
         {
             T* const out = static_cast<T*>(g.d_x) + row * g.d_x_ld;
             const int x_columns = g.d_x ? columns : 0;

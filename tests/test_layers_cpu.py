@@ -23,7 +23,7 @@ def _dropout(lib, **kw):
 
 
 @pytest.mark.parametrize("kw", [dict(device=-1), dict(type=3), dict(type=-1), dict(rows=-1), dict(cols=0), dict(x=None), dict(y=None), dict(x_ld=7), dict(y_ld=7),
-                                dict(residual=P, residual_ld=7), dict(p=-1e-9), dict(p=1.0000001), dict(p=float("nan")), dict(first_row=-1),
+                                dict(residual=P, residual_ld=7), dict(x=P + 2), dict(y=P + 1), dict(type=1, x=P + 1), dict(x_ld=2 ** 39), dict(p=-1e-9), dict(p=1.0000001), dict(p=float("nan")), dict(first_row=-1),
                                 dict(first_row=2 ** 32 - 3), dict(rows=2 ** 32 + 1)])
 def test_dropout(lib, kw):
     assert _dropout(lib, **kw) == binding.ERR_BAD_ARG
@@ -43,7 +43,7 @@ def _layer(**kw):
     return binding.NormLayer(*a.values())
 
 
-BAD_LAYERS = [dict(rows=-1), dict(rows=2 ** 31), dict(cols=0), dict(type=7), dict(x=None), dict(x_ld=7), dict(h_ld=7), dict(gate=P, gate_ld=7), dict(gate=P, gate_ld=8, gate_rows=0),
+BAD_LAYERS = [dict(rows=-1), dict(rows=2 ** 30 + 1), dict(x=P + 2), dict(h=P + 1), dict(scale=P + 2), dict(pre_bias=P + 1), dict(x_ld=2 ** 39), dict(cols=0), dict(type=7), dict(x=None), dict(x_ld=7), dict(h_ld=7), dict(gate=P, gate_ld=7), dict(gate=P, gate_ld=8, gate_rows=0),
               dict(gate_kind=3), dict(gate_kind=-1), dict(post=3), dict(pre=-1), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")),
               dict(h=None, scale=P), dict(h=None, gate=P, gate_ld=8), dict(h=None, post_weight=P), dict(h=None, post_bias=P)]
 
@@ -88,15 +88,18 @@ def test_norm_gradients(lib):
 def test_products(lib):
     def quantize(device=0, type=0, rows=4, cols=8, x=P, x_ld=8, q=P, q_ld=8, scale=P):
         return lib.cutoff_quantize_rows(device, type, rows, cols, x, x_ld, q, q_ld, scale, None)
-    for kw in (dict(device=-1), dict(type=3), dict(rows=-1), dict(rows=2 ** 31), dict(cols=0), dict(x=None), dict(q=None), dict(scale=None), dict(x_ld=7), dict(q_ld=7)):
+    for kw in (dict(device=-1), dict(type=3), dict(rows=-1), dict(rows=2 ** 31), dict(cols=0), dict(x=None), dict(q=None), dict(scale=None), dict(x_ld=7), dict(q_ld=7), dict(x=P + 2), dict(scale=P + 2)):
         assert quantize(**kw) == binding.ERR_BAD_ARG, kw
 
     def product(device=0, m=4, n=8, k=16, a=P, a_ld=16, a_scale=P, b=P, b_ld=16, b_scale=P, bias=None, type=0, y=P, y_ld=8):
         return lib.cutoff_quantized_product(device, m, n, k, a, a_ld, a_scale, b, b_ld, b_scale, bias, type, y, y_ld, None)
     for kw in (dict(device=-1), dict(m=-1), dict(m=2 ** 31), dict(n=0), dict(k=0), dict(a=None), dict(a_scale=None), dict(b=None), dict(b_scale=None), dict(type=5), dict(y=None),
-               dict(a_ld=15), dict(b_ld=24), dict(y_ld=7), dict(a=P + 8), dict(b=P + 1)):
+               dict(a_ld=15), dict(b_ld=24), dict(y_ld=7), dict(a=P + 8), dict(b=P + 1), dict(y=P + 2), dict(bias=P + 2), dict(b_ld=2 ** 39)):
         assert product(**kw) == binding.ERR_BAD_ARG, kw
     assert product(k=131072, a_ld=131072, b_ld=131072) == binding.ERR_TOO_LARGE
+    assert product(n=2 ** 30 + 1, y_ld=2 ** 31) == binding.ERR_TOO_LARGE
+    assert quantize(cols=2 ** 30 + 1, x_ld=2 ** 31, q_ld=2 ** 31) == binding.ERR_TOO_LARGE
+    assert _dropout(lib, cols=2 ** 30 + 1, x_ld=2 ** 31, y_ld=2 ** 31) == binding.ERR_TOO_LARGE
 
 
 def test_longest_sum_fits_32_bits():
