@@ -60,11 +60,12 @@ bool launch_norm(const NormArgs& a, int sms, cudaStream_t s) {
         ops.slot_bytes = slot_bytes_of(ops.row_bytes, SIZE ? SIZE : threads, VV * K, kSize, VV > 1);
         const int stage = kTeamsHere<SIZE> * ops.n * ops.slot_bytes, by_registers = 65536 / (threads * (bias || groups ? kNormRegisters<VV, K, true> : kNormRegisters<VV, K, false>)), most = by_registers < 16 ? by_registers : 16;
         const int ctas = ceil_div(a.rows, kTeamsHere<SIZE>);
-        Staging st = staging(most, stage, 0);
-        if (ctas <= sms * st.per_sm) st.stages = 1, st.bytes = stage;         // a row each
+        const int gate = groups ? kTeamsHere<SIZE> * (SIZE ? SIZE : threads) * VV * K * 4 : 0;
+        Staging st = staging(most, stage, gate);
+        if (ctas <= sms * st.per_sm) st.stages = 1, st.bytes = stage + gate;  // a row each
         ops.stages = st.stages;
         if (st.bytes > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, st.bytes) != cudaSuccess) return;
-        kernel<<<ctas < sms * st.per_sm ? ctas : sms * st.per_sm, threads, st.bytes, s>>>(a, ops);
+        kernel<<<ctas < sms * st.per_sm ? ctas : sms * st.per_sm, threads, st.bytes, s>>>(a, ops, st.stages * stage);
         ok = true;
     });
     return ok;
@@ -88,9 +89,9 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
         ops.row_bytes = g.f.cols * kSize;
         ops.slot_bytes = slot_bytes_of(ops.row_bytes, SIZE ? SIZE : plan.threads, V * K, kSize, V > 1);
         const int stage = kTeamsHere<SIZE> * ops.n * ops.slot_bytes,
-                  params = (BIAS ? 3 : 2) * 4 * (SIZE ? SIZE : plan.threads) * V * K;
+                  columns = (SIZE ? SIZE : plan.threads) * V * K, params = (BIAS ? 3 : 2) * 4 * columns, gate = GROUPS ? kTeamsHere<SIZE> * 4 * columns : 0;
         // the plan's CTAs are resident by their registers; where shared memory holds fewer, the others follow
-        Staging st = staging(plan.per_sm, stage, params);
+        Staging st = staging(plan.per_sm, stage, params + gate);
         const bool layer = g.f.post == kNormLayer || g.f.pre == kNormLayer;
         auto kernel = layer ? k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, true, true> : k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, false, true>;
         if constexpr (sizeof(T) == 4 && V * K == 16 && SIZE == 0)
@@ -99,7 +100,8 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
                 kernel = layer ? k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, true, false> : k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, false, false>;
             }
         ops.stages = st.stages;
-        g.param_bytes = st.stages * stage;
+        g.gate_bytes = st.stages * stage;
+        g.param_bytes = st.stages * stage + gate;
         const int sums = SIZE ? g.f.cols * 4 : 0;
         if (st.bytes < sums) st.bytes = sums;
         if (st.bytes > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, st.bytes) != cudaSuccess) return;

@@ -20,6 +20,7 @@ enum : int { kNormNone = 0, kNormRms = 1, kNormLayer = 2 };
 enum : int { kGateLinear = 0, kGateSigmoid = 1, kGateSilu = 2 };
 
 constexpr int kMostRows = 1 << 30;
+constexpr int kFewCtas = 148;
 
 struct NormArgs {
     const void *x, *h, *gate;                     // h: null = no block before (r = x); gate: null = 1
@@ -203,6 +204,7 @@ constexpr int kTeamsHere = SIZE ? kNormWarpThreads / (SIZE ? SIZE : 1) : 1;
     __shared__ __align__(8) uint64_t barriers[2 * kTeamsHere<SIZE>];                                                             \
     Team<SIZE> team(scratch);                                                                                                    \
     const Columns<SIZE, V, K> col(team, (ARGS).cols);                                                                            \
+    const Columns<SIZE, V, GROUPS ? K : 0> gate_columns(team, (ARGS).cols);                                                      \
     const int team_here = SIZE ? threadIdx.x / (SIZE ? SIZE : 1) : 0;                                                            \
     const RowPipe<T, SIZE> pipe(OPERANDS, async::smem_u32(dynamic), async::smem_u32(barriers), team_here);                       \
     if (team.rank() == 0) pipe.open();                                                                                           \
@@ -220,40 +222,49 @@ __device__ __forceinline__ void take(uint32_t row_at, const Columns<SIZE, V, K>&
     read_shared<T, V, V == 1 || SIZE != 0>(row_at + col(k) * static_cast<int>(sizeof(T)), col(k), columns, f);
 }
 
-// The gate of a group of rows, as a team that goes through the rows in their order keeps it.  Zeros beyond the row (where an infinite gate would turn
-// zeros into NaN).
-template <typename T, int V, int K>
+// act(gate) of a group of rows, in shared memory, formed when a team that goes through the rows in their order comes to the group: a thread
+// writes and reads its own columns.  Zeros beyond the row (where an infinite gate would turn zeros into NaN).
+template <typename T, int V, int K, int SIZE>
 struct GroupGate {
-    Pack<T, V> held[K];
-    int group = -1;
-    __device__ __forceinline__ GroupGate() {      // a team without rows has zeros
+    uint32_t at;                    // this team's [columns of all its threads] fp32
+    const Columns<SIZE, V, K>& col;
+    int group;
+    __device__ __forceinline__ GroupGate(uint32_t smem, int team_here, const Team<SIZE>& team, const Columns<SIZE, V, K>& c)
+        : at(smem + team_here * team.size() * V * K * 4), col(c), group(-1) {
+        put([](int, Num<V> (&u)[kNums<V>]) {      // a team without rows has zeros
 #pragma unroll
-        for (int k = 0; k < K; ++k) held[k] = zero_pack<T, V>();
+            for (int i = 0; i < kNums<V>; ++i) u[i] = splat<Num<V>>(0.f);
+        });
     }
-    template <int SIZE>
-    __device__ __forceinline__ void turn_to(int g, const void* gate, int64_t ld, const Columns<SIZE, V, K>& col) {
-        if (g == group) return;
-        group = g;
-        const T* const row = static_cast<const T*>(gate) + g * ld;
+    template <typename F>
+    __device__ __forceinline__ void put(F f) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            held[k] = zero_pack<T, V>();
-            if (!col.has(k)) continue;
-            if constexpr (V == 1) held[k].v[0] = row[col(k)];
-            else *reinterpret_cast<uint4*>(&held[k]) = __ldg(reinterpret_cast<const uint4*>(row + col(k)));
+            Num<V> u[kNums<V>];
+            f(k, u);
+            if constexpr (V == 1) {
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * col(k)), "f"(u[0].v) : "memory");
+            } else {
+#pragma unroll
+                for (int i = 0; i < V / 2; i += 2) asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(at + 4 * col(k) + 8 * i), "l"(u[i].v), "l"(u[i + 1].v) : "memory");
+            }
         }
     }
-    __device__ __forceinline__ void get(int k, Num<V> (&f)[kNums<V>]) const {
-        if constexpr (V == 1) {
-            f[0].v = to_float(held[k].v[0]);
-        } else if constexpr (sizeof(T) == 4) {
-            f[0].v = pack2(held[k].v[0], held[k].v[1]);
-            f[1].v = pack2(held[k].v[2], held[k].v[3]);
-        } else {
-            const uint4 t = *reinterpret_cast<const uint4*>(&held[k]);
-            f[0] = pair_of<T>(t.x); f[1] = pair_of<T>(t.y); f[2] = pair_of<T>(t.z); f[3] = pair_of<T>(t.w);
-        }
+    __device__ __forceinline__ void turn_to(int g, const NormArgs& a) {
+        if (g == group) return;
+        group = g;
+        const T* const row = static_cast<const T*>(a.gate) + g * a.gate_ld;
+        with_gate(a.gate_kind, [&](auto kind) {
+            put([&](int k, Num<V> (&u)[kNums<V>]) {
+                read_global<T, V>(row + (col.has(k) ? col(k) : 0), u);
+                gate_values<decltype(kind)::value, false>(u, u);
+                if (!col.has(k))
+#pragma unroll
+                    for (int i = 0; i < kNums<V>; ++i) u[i] = splat<Num<V>>(0.f);
+            });
+        });
     }
+    __device__ __forceinline__ void get(int k, Num<V> (&f)[kNums<V>]) const { read_shared_params<V>(at + 4 * col(k), f); }
 };
 // Rows of team t where the teams' rows are consecutive.
 __device__ __forceinline__ int first_row_of(int t, int teams, int rows) { return rows / teams * t + min(t, rows % teams); }
@@ -275,10 +286,12 @@ constexpr int kNormRegisters = V * K > 8 ? (MORE ? 112 : 80) : (MORE ? 80 : 64);
 // The parameters of a thread's columns stay in its registers: in the L1, beside the operands' shared memory, there is no room for them, and every row
 // would bring them from the L2 again (4096 bf16 values with gate, 16384 rows: 152 us so; 5000 rows of 2175 fp32 values 131).
 template <typename T, int V, int K, int SIZE, bool LAYER, bool BIAS, bool GROUPS>
-__global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands) {
+__global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands, int gate_bytes) {
     using N = Num<V>;
     constexpr int M = kNums<V>, kBias = BIAS ? K : 1;
     CUTOFF_NORM_TEAM(a, operands)
+    // With at most a CTA per SM the successor, a product of few tokens perhaps, may set itself up meanwhile; the CTAs of a large one would crowd on some SMs.
+    if (gridDim.x <= kFewCtas) launch_dependents();
     const int at_h = 1, at_gate = 2;
     const int t = blockIdx.x * kTeamsHere<SIZE> + team_here, teams = gridDim.x * kTeamsHere<SIZE>;
     const TeamRows<GROUPS> rows(t, teams, a.rows);
@@ -286,7 +299,7 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
     bool failed = false;                          // a wait gave up: none is made after it, and nothing is asked for
     for (int s = 0; s < operands.stages; ++s)
         if (rows.has(s)) pipe.fetch(s, rows(s), team);
-    GroupGate<T, V, GROUPS ? K : 1> group_gate;
+    GroupGate<T, V, GROUPS ? K : 0, SIZE> group_gate(async::smem_u32(dynamic) + gate_bytes, team_here, team, gate_columns);
     N post_w[K][M], pre_w[K][M], post_b[kBias][M] = {}, pre_b[kBias][M] = {};       // the block's scale is part of the first and the third
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -309,7 +322,7 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
         const int columns = !SIZE || mine ? a.cols : 0;
         if (!SIZE && !mine) break;
         if constexpr (GROUPS)
-            if (mine) group_gate.turn_to(row / a.gate_rows, a.gate, a.gate_ld, col);
+            if (mine) group_gate.turn_to(row / a.gate_rows, a);
         failed = failed || (mine && !pipe.wait(turn));
         const uint32_t x_at = pipe.template row_at<V>(stage, 0, row);
         N r[K][M];
@@ -333,13 +346,19 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_n
                 for (int i = 0; i < M; ++i) r[k][i] = fma(r[k][i], t[i], x[i]);
                 write_global<T, V>(r_row, col(k), r_columns, r[k]);
             };
-            if (a.gate) {
+            if constexpr (GROUPS) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    N t[M];
+                    group_gate.get(k, t);
+                    add_x(k, t);
+                }
+            } else if (a.gate) {
                 with_gate(a.gate_kind, [&](auto kind) {
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
                         N t[M];
-                        if constexpr (GROUPS) group_gate.get(GROUPS ? k : 0, t);
-                        else take<T, V>(gate_at, col, k, columns, t);
+                        take<T, V>(gate_at, col, k, columns, t);
                         gate_values<decltype(kind)::value, false>(t, t);
                         add_x(k, t);
                     }
@@ -405,6 +424,7 @@ struct NormGradArgs {
     float* sums;                                  // [CTAs][2 or 4][cols]: sum e * hat, sum d_n * r_hat, with BIAS also sum e, sum d_n
     float* gate_sums;                             // [teams][2][cols]: of the team's first and last group, where another team has the rest
     int teams;
+    int gate_bytes;                               // offset in shared memory of the teams' group gates
     int param_bytes;                              // offset in shared memory of the parameters: scale * post_w, pre_w, with BIAS scale * post_b
 };
 constexpr int kGradThreads = 512;                 // most threads of a CTA: 128 registers each
@@ -424,7 +444,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
     const TeamRows<GROUPS> rows(t, g.teams, a.rows);
     const int turns = ceil_div(a.rows, g.teams);               // the same for all teams of a warp: its shuffles take all lanes
     constexpr int kBias = BIAS ? K : 1, kGroups = GROUPS ? K : 1;
-    GroupGate<T, V, GROUPS ? K : 1> group_gate;
+    GroupGate<T, V, GROUPS ? K : 0, SIZE> group_gate(async::smem_u32(dynamic) + g.gate_bytes, team_here, team, gate_columns);
     N e_hat[K][M] = {}, n_hat[K][M] = {}, e_sum[kBias][M] = {}, n_sum[kBias][M] = {}, gate_sum[kGroups][M] = {};
 
     // places of the operands in a stage
@@ -486,12 +506,8 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
         failed = failed || (mine && !pipe.wait(turn));
         const int group = GROUPS && mine ? row / a.gate_rows : 0;
         if constexpr (GROUPS)
-            if (mine) group_gate.turn_to(group, a.gate, a.gate_ld, col);
+            if (mine) group_gate.turn_to(group, a);
         const uint32_t gate_at = has_gate_rows ? pipe.template row_at<V>(stage, at_gate, row) : 0u;
-        const auto gate_of = [&](int k, N (&u)[M]) {
-            if constexpr (GROUPS) group_gate.get(GROUPS ? k : 0, u);
-            else take<T, V>(gate_at, col, k, columns, u);
-        };
         N hat[K][M], d[K][M];                     // d: the whole gradient at r
         float h_inv = 1.f;
         if (a.h) {
@@ -524,12 +540,19 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
 #pragma unroll
                     for (int i = 0; i < M; ++i) r[k][i] = fma(r[k][i], t[i], x[i]);
                 };
-                if (a.gate) {
+                if constexpr (GROUPS) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        N t[M];
+                        group_gate.get(k, t);
+                        add_x(k, t);
+                    }
+                } else if (a.gate) {
                     with_gate(a.gate_kind, [&](auto kind) {
 #pragma unroll
                         for (int k = 0; k < K; ++k) {
                             N t[M];
-                            gate_of(k, t);
+                            take<T, V>(gate_at, col, k, columns, t);
                             gate_values<decltype(kind)::value, false>(t, t);
                             add_x(k, t);
                         }
@@ -595,7 +618,31 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                     d[k][i] = mul(d[k][i], w[i]);
                 }
             };
-            if (a.gate) {
+            // the branch behind its scale, scale * post(h), of which the gate's gradient is a multiple
+            const auto branch_of = [&](int k, const N (&w)[M], N (&p)[M]) {
+#pragma unroll
+                for (int i = 0; i < M; ++i) p[i] = mul(hat[k][i], w[i]);
+                if constexpr (BIAS) {
+                    N b[M];
+                    param_of(2, k, b);
+#pragma unroll
+                    for (int i = 0; i < M; ++i) p[i] = add(p[i], b[i]);
+                }
+            };
+            if constexpr (GROUPS) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    N w[M], u[M], p[M];
+                    param_of(0, k, w);
+                    group_gate.get(k, u);
+                    branch_of(k, w, p);
+#pragma unroll
+                    for (int i = 0; i < M; ++i) gate_sum[k][i] = fma(d[k][i], p[i], gate_sum[k][i]);
+#pragma unroll
+                    for (int i = 0; i < M; ++i) d[k][i] = mul(d[k][i], u[i]);
+                    at_hat(k, w);
+                }
+            } else if (a.gate) {
                 T* const gate_row = static_cast<T*>(g.d_gate) + row * g.d_gate_ld;
                 const int gate_columns = g.d_gate ? columns : 0;
                 with_gate(a.gate_kind, [&](auto kind) {
@@ -603,24 +650,12 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                     for (int k = 0; k < K; ++k) {
                         N w[M], u[M], slope[M], p[M];
                         param_of(0, k, w);
-                        gate_of(k, u);
-                        gate_values<decltype(kind)::value, !GROUPS>(u, slope);
+                        take<T, V>(gate_at, col, k, columns, u);
+                        gate_values<decltype(kind)::value, true>(u, slope);
+                        branch_of(k, w, p);
 #pragma unroll
-                        for (int i = 0; i < M; ++i) p[i] = mul(hat[k][i], w[i]);
-                        if constexpr (BIAS) {
-                            N b[M];
-                            param_of(2, k, b);
-#pragma unroll
-                            for (int i = 0; i < M; ++i) p[i] = add(p[i], b[i]);
-                        }
-                        if constexpr (GROUPS) {
-#pragma unroll
-                            for (int i = 0; i < M; ++i) gate_sum[k][i] = fma(d[k][i], p[i], gate_sum[k][i]);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], mul(d[k][i], p[i]));
-                            write_global<T, V>(gate_row, col(k), gate_columns, slope);
-                        }
+                        for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], mul(d[k][i], p[i]));
+                        write_global<T, V>(gate_row, col(k), gate_columns, slope);
 #pragma unroll
                         for (int i = 0; i < M; ++i) d[k][i] = mul(d[k][i], u[i]);
                         at_hat(k, w);
@@ -658,7 +693,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
                         if (col.has(k)) {
                             if (whole) {
                                 N u[M], slope[M];
-                                gate_of(k, u);
+                                read_global<T, V>(static_cast<const T*>(a.gate) + group * a.gate_ld + col(k), u);
                                 with_gate(a.gate_kind, [&](auto kind) { gate_values<decltype(kind)::value, true>(u, slope); });
 #pragma unroll
                                 for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], gate_sum[k][i]);
@@ -675,6 +710,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ?
         }
     }
     if (failed) pipe.drain();
+    launch_dependents();                          // the kernel that adds the sums up may set itself up
     // this CTA's sums
     float* const out = g.sums + static_cast<int64_t>(blockIdx.x) * (BIAS ? 4 : 2) * a.cols;
     float* const column_sums = reinterpret_cast<float*>(dynamic);
