@@ -4,4 +4,5 @@
 `inputs` draws the seeded synthetic weights and run-time traces.
 """
 from . import binding, inputs  # noqa: F401
-from .binding import Cutoff, CutoffError, debug_normals, load_library, pack_weights  # noqa: F401
+from .binding import (Cutoff, CutoffError, debug_normals, dropout, load_library, pack_weights, quantize_rows,  # noqa: F401
+                      quantized_product, residual_norm, residual_norm_grad)

@@ -8,6 +8,9 @@
 // A thread owns eight consecutive columns, one generator call, and walks down the rows, so that what the first rounds compute from
 // the column alone is computed once per thread (philox_column): the ten rounds are the longest part of the instructions, and 16 bits
 // per value instead of 32 halve them.
+//
+// What bounds it is the memory, and next to it the issue slots (some fifteen instructions per value): 16384 x 4096 bf16 with a residual 72 us, 0.40 GB, 85 %
+// of a copy's rate; 8001 x 2175 fp32, rows that are not aligned, 26 us (81 %).  Two rows of a thread at a time with bounds checks on each took 96 and 33.
 #pragma once
 #include "layer_types.cuh"
 #include "rng.cuh"

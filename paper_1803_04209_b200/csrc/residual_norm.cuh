@@ -7,9 +7,17 @@
 // it is stored.  The backward pass reads x and h, not r: the parameters' gradients are fp32 sums, and a rounded r would be seen in them.
 // It forms the statistics again instead of reading them: the rows are in registers anyway.
 //
-// A row belongs to a team, 4 to 32 lanes of a warp (rows of up to 512 values) or a CTA.  Forward: one row per team.  Backward:
-// each team walks over consecutive rows and keeps the parameters' sums of its columns in registers; k_norm_grad_finish adds the CTAs' sums
-// in their order, so that results are the same on every run.
+// A row belongs to a team, 4 to 32 lanes of a warp (rows of up to 512 values) or a CTA, that goes through many rows; the asynchronous copy engine brings
+// the operands of the next row into shared memory meanwhile (RowPipe).  The backward pass keeps the parameters' sums of a thread's columns in
+// registers; k_norm_grad_finish adds the CTAs' sums in their order, so that results are the same on every run.
+//
+// What bounds it (4096 bf16 values, 16384 rows, a gate value for each): the forward pass the memory, 0.67 GB in 108 us, 95 % of a copy's rate; the
+// backward pass, 1.07 GB in 224 us (73 %), its instructions, some 55 per value and as many as 16 warps of 128 registers issue between three sums
+// over the CTA per row.  What made it so, in us: operands in registers 341 and 703; staged by cp.async 157 and 357; by bulk copies, with two values per
+// instruction and parameters in registers or shared memory (in the L1, beside the operands, there is no room for them) 153 and 281; predicates beside the accesses and one branch
+// on the gate's kind per row instead of one for each pack 108 and 224.  Odd rows pay for single values: 5000 rows of 2175 fp32 values with
+// layer norms, biases and a gate for every 125 rows 54 to 60 us (floor 27), the gradients of 4001 x 1025 63 us (floor 15).  Not kept: consecutive rows per team
+// where nothing asks for them (150 us against 106).
 #pragma once
 #include "layer_types.cuh"
 
@@ -283,8 +291,7 @@ struct TeamRows {
 template <int V, int K, bool MORE>
 constexpr int kNormRegisters = V * K > 8 ? (MORE ? 112 : 80) : (MORE ? 80 : 64);
 
-// The parameters of a thread's columns stay in its registers: in the L1, beside the operands' shared memory, there is no room for them, and every row
-// would bring them from the L2 again (4096 bf16 values with gate, 16384 rows: 152 us so; 5000 rows of 2175 fp32 values 131).
+// The parameters of a thread's columns stay in its registers.
 template <typename T, int V, int K, int SIZE, bool LAYER, bool BIAS, bool GROUPS>
 __global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands, int gate_bytes) {
     using N = Num<V>;
@@ -809,9 +816,9 @@ __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_fi
     if (q.d_pre_b) q.d_pre_b[c] = s[3];
 }
 
-// The teams of a backward pass: their threads (32 lanes or fewer, or a CTA), the values of a thread, the CTAs.  Without more sums than the two products
-// a thread has room for 16 values (rows of 4096 bf16 values 719 us with eight and operands in registers, ...); with them it has eight, where a CTA can then
-// hold a row at all.
+// The teams of a backward pass: their threads (32 lanes or fewer, or a CTA), the values of a thread, the CTAs.  A thread has sixteen values where its sums then fit
+// its registers: two each of a CTA's 128, with groups or biases up to five in a warp team's 168 (100000 rows of 512 fp16 values with groups: 178 us so,
+// 217 with eight in CTAs of two warps).  Otherwise eight, as fp32 rows, which would leave a CTA of 16 values half of its warps.
 struct GradPlan {
     int lanes, values, threads, per_sm, ctas, teams;
 };
