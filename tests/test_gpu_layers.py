@@ -194,3 +194,38 @@ def test_two_graphs_and_an_eager_call_at_once():
         torch.cuda.synchronize()
         for out in (graphs[0][1], graphs[1][1], eager):
             assert all(torch.equal(out[k], want[k]) for k in want)
+
+
+# ---- the very first calls of a process, captured: nothing is set up by them that a capture would not allow ---------------------------
+FIRST = """
+import sys
+sys.path.insert(0, {root!r})
+import torch
+from paper_1803_04209_b200 import binding
+x = torch.randn(100, 520, device="cuda", dtype=torch.bfloat16)
+w = binding.Quantized(torch.randint(-127, 128, (640, 528), dtype=torch.int8, device="cuda")[:, :520], torch.rand(640, device="cuda"))
+v = torch.ones(520, device="cuda")
+torch.cuda.synchronize()
+def calls():
+    y = binding.dropout(x, 0.5, 1, residual=x)
+    r, n = binding.residual_norm(x, y, scale=v, post_weight=v, pre_weight=v)
+    g = binding.residual_norm_grad(x, y, r, n, scale=v, post_weight=v, pre_weight=v)
+    _, q = binding.residual_norm(x, y, quantize=True)
+    return [y, r, n, *g.values(), binding.quantized_product(q, w), binding.quantized_product(binding.quantize_rows(x[:1]), w)]
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    held = calls()
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(held, calls()))
+print("captured")
+"""
+
+
+def test_first_calls_may_be_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST.format(root=root)], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "captured" in done.stdout, done.stderr[-2000:]

@@ -62,7 +62,8 @@ def _case(rng, rows, cols, dt, post="rms", pre="rms", gate_rows=None, gate_kind=
     return (x, h, {**dev, **rest}), (x64, h64, {**none, **ref, **rest})
 
 
-SIZES = [(1, 1), (3, 5), (2, 32), (70, 33), (5, 128), (9, 129), (3, 256), (40, 257), (2, 512), (6, 513), (3, 1000), (600, 1024), (2, 2175), (1, 4096), (3, 8192), (2, 8191)]
+SIZES = [(1, 1), (3, 5), (2, 32), (70, 33), (5, 128), (9, 129), (3, 256), (40, 257), (2, 512), (6, 513), (3, 1000), (600, 1024), (2, 2175), (1, 4096), (3, 8192), (2, 8191),
+         (520, 2175), (513, 8192), (900, 1001), (2100, 100), (1500, 516)]
 
 
 # both sides of every length at which another number of threads takes a row
@@ -153,7 +154,7 @@ def test_in_place():
 
 # the 8-bit rows are those that quantising the unrounded fp32 rows gives, up to values that lie on a border between two integers
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("rows,cols", [(1, 16), (7, 100), (3, 300), (2, 1000), (1, 4096), (5, 8192), (4, 2175)])
+@pytest.mark.parametrize("rows,cols", [(1, 16), (7, 100), (3, 300), (2, 1000), (1, 4096), (5, 8192), (4, 2175), (700, 1024), (600, 1001), (3000, 48)])
 def test_rows_in_8_bits(dtype, rows, cols):
     rng = np.random.default_rng(cols)
     dt = TYPES[dtype]

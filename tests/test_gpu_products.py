@@ -61,7 +61,7 @@ def _bound(want, total, a_scale, b_scale, bias, dt):
 SIZES = [(1, 1, 1), (1, 8, 16), (2, 5, 17), (1, 300, 4096), (3, 129, 130), (8, 128, 512), (9, 64, 100), (16, 256, 128), (17, 200, 1000), (33, 130, 33),
          (64, 1024, 256), (64, 9600, 384), (65, 127, 129), (128, 128, 128), (129, 257, 640), (200, 513, 1001), (256, 256, 2048), (257, 600, 96), (300, 8, 48), (1000, 130, 272),
          (2, 2048, 8192), (48, 640, 8192), (100, 2175, 513), (1024, 1024, 512), (300, 512, 4096), (200, 5000, 640),
-         (1300, 2300, 200), (4000, 2000, 129)]
+         (1300, 2300, 200), (4000, 2000, 129), (20, 6000, 300), (31, 5000, 2000), (100, 4000, 1024), (5, 1, 40), (128, 128, 4096)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
