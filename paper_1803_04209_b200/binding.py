@@ -603,6 +603,14 @@ def _same(t, what: str, rows: int, cols: int, device: int, dtype):
     return at, ld
 
 
+def _result(x, out, what: str, rows: int, cols: int, device: int, dtype):
+    """(tensor, address, leading dimension) of a result like x: `out`, or a new matrix."""
+    if out is None:
+        out = _torch.empty_like(x, memory_format=_torch.contiguous_format)
+        return out, out.data_ptr() or 16, cols
+    return out, *_same(out, what, rows, cols, device, dtype)
+
+
 def _vector(t, what: str, n: int, device: int) -> int:
     if t is None:
         return 0
@@ -621,13 +629,12 @@ def dropout(x, p: float, seed: int, step: int = 0, noise_stream: int = STREAM_DR
 
     The gradient with respect to x is dropout(gradient of the result, p, seed, step, noise_stream, first_row); that with respect to the
     residual is the gradient of the result.  p counts in steps of 2^-16.  out may be x or residual."""
-    torch, lib = _load_torch(), load_library()
+    lib = load_library()
+    _load_torch()
     xp, x_ld, rows, cols, device, dtype = _matrix(x, "x")
     code = _type_of(dtype)
-    if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
     rp, r_ld = _same(residual, "residual", rows, cols, device, dtype)
-    op, o_ld = _same(out, "out", rows, cols, device, dtype)
+    out, op, o_ld = _result(x, out, "out", rows, cols, device, dtype)
     if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= noise_stream < 1 << 32):
         raise ValueError("seed has 64 bits, step and noise_stream 32")
     rc = lib.cutoff_dropout(device, code, rows, cols, xp, x_ld, rp, r_ld, op, o_ld, p, seed, step, noise_stream, first_row, _current_stream(device))
@@ -660,17 +667,16 @@ def residual_norm(x, h=None, gate=None, gate_rows: int = 1, gate_kind: str = "li
     x, h [rows, cols]; gate [ceil(rows / gate_rows), cols]; post, pre: "rms", "layer" or None, with weights and biases [cols].  Without h there is no
     block before: r is x.  With want_norm=False n is None.  With quantize=True n is a Quantized of 8-bit rows, as quantized_product takes them.
     residual_out and norm_out may be x or h."""
-    torch, lib = _load_torch(), load_library()
+    lib = load_library()
+    _load_torch()
     layer, rows, cols, device, dtype = _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps)
     r, rp, r_ld, n, np_, n_ld, sp = x, None, 0, None, None, 0, None
     if h is not None:
-        r = torch.empty_like(x, memory_format=torch.contiguous_format) if residual_out is None else residual_out
-        rp, r_ld = _same(r, "residual_out", rows, cols, device, dtype)
+        r, rp, r_ld = _result(x, residual_out, "residual_out", rows, cols, device, dtype)
     if want_norm and quantize:
         n, np_, n_ld, sp = _empty_quantized(x, rows, cols)
     elif want_norm:
-        n = torch.empty_like(x, memory_format=torch.contiguous_format) if norm_out is None else norm_out
-        np_, n_ld = _same(n, "norm_out", rows, cols, device, dtype)
+        n, np_, n_ld = _result(x, norm_out, "norm_out", rows, cols, device, dtype)
     rc = lib.cutoff_residual_norm(device, layer, rp, r_ld, np_, n_ld, sp, _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_residual_norm")

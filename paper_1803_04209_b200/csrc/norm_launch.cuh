@@ -58,7 +58,7 @@ bool launch_norm(const NormArgs& a, int sms, cudaStream_t s) {
         if (a.gate && a.gate_rows == 1) use(a.gate, a.gate_ld);
         ops.row_bytes = a.cols * kSize;
         ops.slot_bytes = slot_bytes_of(ops.row_bytes, SIZE ? SIZE : threads, VV * K, kSize, VV > 1);
-        const int stage = kTeamsHere<SIZE> * ops.n * ops.slot_bytes, by_registers = 65536 / (threads * (bias || groups ? kNormRegisters<VV, K, true> : kNormRegisters<VV, K, false>)), most = by_registers < 16 ? by_registers : 16;
+        const int stage = kTeamsHere<SIZE> * ops.n * ops.slot_bytes, by_registers = 65536 / (threads * (bias ? kNormRegisters<VV, K, true> : kNormRegisters<VV, K, false>)), most = by_registers < 16 ? by_registers : 16;
         const int ctas = ceil_div(a.rows, kTeamsHere<SIZE>);
         const int gate = groups ? kTeamsHere<SIZE> * (SIZE ? SIZE : threads) * VV * K * 4 : 0;
         Staging st = staging(most, stage, gate);

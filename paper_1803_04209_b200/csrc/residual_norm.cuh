@@ -289,11 +289,11 @@ struct TeamRows {
 
 // Registers of a forward thread: with 16 values and their parameters 80, three CTAs of 256 threads per SM.
 template <int V, int K, bool MORE>
-constexpr int kNormRegisters = V * K > 8 ? (MORE ? 112 : 80) : (MORE ? 80 : 64);
+constexpr int kNormRegisters = V * K > 8 ? (MORE ? 96 : 80) : (MORE ? 80 : 64);
 
 // The parameters of a thread's columns stay in its registers.
 template <typename T, int V, int K, int SIZE, bool LAYER, bool BIAS, bool GROUPS>
-__global__ void __maxnreg__((kNormRegisters<V, K, BIAS || GROUPS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands, int gate_bytes) {
+__global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands, int gate_bytes) {
     using N = Num<V>;
     constexpr int M = kNums<V>, kBias = BIAS ? K : 1;
     CUTOFF_NORM_TEAM(a, operands)
