@@ -16,8 +16,8 @@
 // over the CTA per row.  What made it so, in us: operands in registers 341 and 703; staged by cp.async 157 and 357; by bulk copies, with two values per
 // instruction and parameters in registers or shared memory (in the L1, beside the operands, there is no room for them) 153 and 281; predicates beside the accesses and one branch
 // on the gate's kind per row instead of one for each pack 108 and 224.  Odd rows pay for single values: 5000 rows of 2175 fp32 values with
-// layer norms, biases and a gate for every 125 rows 54 to 60 us (floor 27), the gradients of 4001 x 1025 63 us (floor 15).  Not kept: consecutive rows per team
-// where nothing asks for them (150 us against 106).
+// layer norms, biases and a gate for every 125 rows 53 us (floor 27), the gradients of 4001 x 1025 63 us (floor 15).  Not kept: consecutive rows per team
+// where nothing asks for them (150 us against 106); single values in pairs a team apart, two to an instruction (no gain: latency bounds those rows).
 #pragma once
 #include "layer_types.cuh"
 

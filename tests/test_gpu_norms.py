@@ -254,6 +254,21 @@ def test_gradients_of_shared_gates(rows, cols, gate_rows, dtype):
     _grad_check(*dev, *ref, TYPES[dtype])
 
 
+# the most shared memory that a row takes: every operand, bias and group at the largest widths
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,cols", [(5, 8192), (700, 8184), (3, 8190)])
+@pytest.mark.parametrize("gate_rows", [1, 3])
+def test_widest_rows(dtype, rows, cols, gate_rows):
+    rng = np.random.default_rng(cols + gate_rows)
+    dt = TYPES[dtype]
+    dev, ref = _case(rng, rows, cols, dt, post="layer", gate_rows=gate_rows, gate_kind="silu", eps=1e-2)
+    d, b_r, b_n = _forward_bounds(*ref, dt)
+    r, n = binding.residual_norm(*dev[:2], **dev[2])
+    close(r, d["r"], b_r, "r")
+    close(n, d["n"], b_n, "n")
+    _grad_check(*dev, *ref, dt)
+
+
 @pytest.mark.parametrize("with_r,with_n", [(True, False), (False, True)])
 @pytest.mark.parametrize("cols", [100, 1024])
 def test_one_of_the_gradients_may_be_absent(with_r, with_n, cols):
