@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
 #pragma unroll 2
             for (int c0 = 0; c0 < BN; c0 += 16) {
                 uint32_t r[16];
+                __syncwarp();                     // lanes without a channel went on earlier
                 tc::tmem_ld16(lanes + c0, r);
                 tc::tmem_ld_wait();
 #pragma unroll

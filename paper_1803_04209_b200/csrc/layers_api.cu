@@ -57,14 +57,16 @@ constexpr int kMostProductCols = 1 << 30;     // of dropout, quantised rows and 
 // ---- dropout ---------------------------------------------------------------------------------------------------------
 template <typename T, int V, int LX>
 void launch_dropout(const DropoutArgs& a, int sms, cudaStream_t s) {
-    constexpr int kUnroll = sizeof(T) == 2 ? 3 : 2, kWarps = kDropoutThreads / 32;
-    const int64_t row_warps = ceil_div64(a.rows, kUnroll * (32 / LX));     // warps that find work in a tile of columns
+    // rows of a thread on their way: as many as fit 80 registers
+    constexpr int kAdd = sizeof(T) == 2 ? 3 : 2, kPlain = V == 1 ? kAdd : sizeof(T) == 2 ? 5 : 3, kWarps = kDropoutThreads / 32;
+    const int unroll = a.residual ? kAdd : kPlain;
+    const int64_t row_warps = ceil_div64(a.rows, unroll * (32 / LX));     // warps that find work in a tile of columns
     const int64_t resident = static_cast<int64_t>(sms) * 3 * kWarps;
     int64_t each = resident / a.tiles;
     each = each < 1 ? 1 : each < row_warps ? each : row_warps;
     const unsigned grid = static_cast<unsigned>(ceil_div64(each * a.tiles, kWarps));
-    if (a.residual) k_dropout<T, V, LX, kUnroll, true><<<grid, kDropoutThreads, 0, s>>>(a);
-    else k_dropout<T, V, LX, kUnroll, false><<<grid, kDropoutThreads, 0, s>>>(a);
+    if (a.residual) k_dropout<T, V, LX, kAdd, true><<<grid, kDropoutThreads, 0, s>>>(a);
+    else k_dropout<T, V, LX, kPlain, false><<<grid, kDropoutThreads, 0, s>>>(a);
 }
 template <typename T, int V>
 void launch_dropout(DropoutArgs& a, int sms, cudaStream_t s) {

@@ -93,11 +93,18 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
         // the plan's CTAs are resident by their registers; where shared memory holds fewer, the others follow
         Staging st = staging(plan.per_sm, stage, params + gate);
         const bool layer = g.f.post == kNormLayer || g.f.pre == kNormLayer;
-        auto kernel = layer ? k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, true, true> : k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, false, true>;
+        // 168 registers where they are needed and the row's threads leave them
+        constexpr int kThreads = V * K == 16 && (BIAS || GROUPS) ? kGradThreadsMany : kGradThreads;
+        auto kernel = layer ? k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, true, true, kThreads> : k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, false, true, kThreads>;
+        if constexpr (SIZE == 0 && kThreads < kGradThreads)
+            if (plan.threads > kThreads)
+                kernel = layer ? k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, true, true, kGradThreads>
+                               : k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, false, true, kGradThreads>;
         if constexpr (sizeof(T) == 4 && V * K == 16 && SIZE == 0)
             if (st.bytes > 225 * 1024) {
                 st.bytes -= params;
-                kernel = layer ? k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, true, false> : k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, false, false>;
+                kernel = layer ? k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, true, false, kGradThreads>
+                               : k_residual_norm_grad<T, V, K, SIZE, BIAS, GROUPS, false, false, kGradThreads>;
             }
         ops.stages = st.stages;
         g.gate_bytes = st.stages * stage;
@@ -116,7 +123,7 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
     else if (plan.lanes == 32 && plan.values == 8) run(eight, integral_constant<int, 32>{});
     else if (plan.lanes == 32) run(sixteen, integral_constant<int, 32>{});
     else if (plan.values == 8) {
-        if constexpr (BIAS || GROUPS || sizeof(T) == 4) run(eight, integral_constant<int, 0>{});
+        if constexpr (sizeof(T) == 4) run(eight, integral_constant<int, 0>{});
     } else run(sixteen, integral_constant<int, 0>{});
     return ok;
 }

@@ -435,14 +435,16 @@ struct NormGradArgs {
     int param_bytes;                              // offset in shared memory of the parameters: scale * post_w, pre_w, with BIAS scale * post_b
 };
 constexpr int kGradThreads = 512;                 // most threads of a CTA: 128 registers each
+constexpr int kGradThreadsMany = 384;             // with 16 values and many sums: 168, where the row allows it
 // CTAs of warp teams per SM: 128 registers for each thread, 168 with 16 values and many sums.
 template <int VALUES, bool MORE>
 constexpr int kGradWarpCtas = VALUES > 8 && MORE ? 3 : 4;
 
 // GROUPS: a gate for each group of rows, whose gradient is a sum over them.  BIAS: either norm has one, so that the plain sums are needed.
 // SHARED: the parameters are in shared memory (there is no room for them beside one row of five fp32 operands of 8192 values).
-template <typename T, int V, int K, int SIZE, bool BIAS, bool GROUPS, bool LAYER, bool SHARED>
-__global__ void __launch_bounds__(SIZE ? kNormWarpThreads : kGradThreads, SIZE ? kGradWarpCtas<V * K, BIAS || GROUPS> : 1) k_residual_norm_grad(NormGradArgs g, const __grid_constant__ RowOperands operands) {
+// THREADS: most threads of a CTA team, and so its registers.
+template <typename T, int V, int K, int SIZE, bool BIAS, bool GROUPS, bool LAYER, bool SHARED, int THREADS>
+__global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGradWarpCtas<V * K, BIAS || GROUPS> : 1) k_residual_norm_grad(NormGradArgs g, const __grid_constant__ RowOperands operands) {
     using N = Num<V>;
     constexpr int M = kNums<V>;
     const NormArgs& a = g.f;
@@ -816,9 +818,9 @@ __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_fi
     if (q.d_pre_b) q.d_pre_b[c] = s[3];
 }
 
-// The teams of a backward pass: their threads (32 lanes or fewer, or a CTA), the values of a thread, the CTAs.  A thread has sixteen values where its sums then fit
-// its registers: two each of a CTA's 128, with groups or biases up to five in a warp team's 168 (100000 rows of 512 fp16 values with groups: 178 us so,
-// 217 with eight in CTAs of two warps).  Otherwise eight, as fp32 rows, which would leave a CTA of 16 values half of its warps.
+// The teams of a backward pass: their threads (32 lanes or fewer, or a CTA), the values of a thread, the CTAs.  A thread has sixteen values; its sums, two each,
+// fit 128 registers, with groups or biases up to five, 168 (100000 rows of 512 fp16 values with groups: 178 us so, 217 with eight values and 128).  Rows of fp32
+// values have eight, as shared memory holds few of them and 16 would leave a CTA half of its warps.
 struct GradPlan {
     int lanes, values, threads, per_sm, ctas, teams;
 };
@@ -826,10 +828,11 @@ constexpr int kMostSms = 160, kMostTeamRows = 1024;          // a team adds at m
 inline GradPlan grad_plan(int rows, int cols, int type_size, bool many_sums, int sms) {
     GradPlan p;
     p.lanes = cols <= 32 ? 4 : cols <= 128 ? 16 : cols <= 512 ? 32 : 0;
-    p.values = p.lanes ? (cols <= 256 ? 8 : 16) : (many_sums || type_size == 4) && cols <= 8 * kGradThreads ? 8 : 16;
+    p.values = p.lanes ? (cols <= 256 ? 8 : 16) : type_size == 4 && cols <= 8 * kGradThreads ? 8 : 16;
     p.threads = p.lanes ? kNormWarpThreads : ceil_div(ceil_div(cols, p.values), 32) * 32;
     // by the registers; shared memory may allow fewer
-    p.per_sm = p.lanes ? (p.values > 8 && many_sums ? kGradWarpCtas<16, true> : kGradWarpCtas<8, false>) : kGradThreads / p.threads;
+    p.per_sm = p.lanes ? (p.values > 8 && many_sums ? kGradWarpCtas<16, true> : kGradWarpCtas<8, false>)
+               : p.values > 8 && many_sums && p.threads <= kGradThreadsMany ? kGradThreadsMany / p.threads : kGradThreads / p.threads;
     const int per_cta = p.lanes ? p.threads / p.lanes : 1;
     const int few = ceil_div(rows, per_cta), many = ceil_div(few, kMostTeamRows), resident = (sms < kMostSms ? sms : kMostSms) * p.per_sm;
     p.ctas = resident < many ? many : resident;
