@@ -58,6 +58,12 @@ struct ProductTile {
 };
 constexpr int kMostSplits = 4;                    // a CTA's share is at least four tokens
 
+// Barrier of the four epilogue warps; it takes whole warps, so their lanes meet first.
+__device__ __forceinline__ void epilogue_sync() {
+    __syncwarp();
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+}
+
 // Bulk copy from this CTA's shared memory to another's, counted on a barrier there.
 __device__ __forceinline__ void bulk_to_cta(uint32_t cluster_dst, uint32_t src, uint32_t bytes, uint32_t cluster_bar) {
     asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -163,7 +169,7 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
         __syncwarp();
     } else {
         for (int c = threadIdx.x - 64; c < BN; c += 128) token_scale[c] = m0 + c < p.m ? p.a_scale[m0 + c] : 0.f;
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        epilogue_sync();
         ok = mbar_wait(acc_full, 0u, abort_flag, none);
         tc::tc_fence_after();
     }
@@ -193,7 +199,7 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
         const int share = BN / splits, piece = share * kProdM;
         if (epilogue) {
             const int lane_at = (quarter * 32 + lane) * 4;
-            const bool good = ok && !*abort_flag;
+            const bool good = !__any_sync(0xffffffffu, !ok || *abort_flag);      // one answer for the warp: reading tensor memory takes all lanes
             if (good) {
 #pragma unroll 2
                 for (int c0 = 0; c0 < BN; c0 += 16) {
@@ -206,11 +212,12 @@ __global__ void __launch_bounds__(192) k_product_tile(const __grid_constant__ CU
                 }
                 fence_proxy_async();
             }
-            asm volatile("bar.sync 1, 128;" ::: "memory");
+            epilogue_sync();
+            const bool sent = !__any_sync(0xffffffffu, !good || *abort_flag);    // all four warps' sums are in the outbox: one that gave up has set the flag
             const int to = threadIdx.x - 64;      // one thread per receiver; a CTA that gave up sends nothing, and the others' waits will too
-            if (good && to < splits && to != split)
+            if (sent && to < splits && to != split)
                 bulk_to_cta(tc::map_to_cta(smem_u32(inbox + split * piece), to), smem_u32(outbox + to * piece), piece * 4, tc::map_to_cta(arrived, to));
-            const bool all = mbar_wait(arrived, 0u, abort_flag, none) && good;
+            const bool all = mbar_wait(arrived, 0u, abort_flag, none) && sent;
             for (int c = 0; c < share; c += 4) {
                 int4 total = *reinterpret_cast<const int4*>(outbox + split * piece + c * kProdM + lane_at);
                 for (int r = 0; r < splits; ++r) {
