@@ -395,7 +395,8 @@ int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const v
  * The gate's gradient has the gate's shape (sums over the rows that share it), its type and all others' but the parameters' is `type`.  The forward pass
  * is not needed before it: r and the statistics are formed again from x and h.  workspace: device, 16-byte aligned, at least
  * cutoff_residual_norm_grad_workspace_bytes(rows, cols) bytes, contents undefined afterwards; calls that may overlap need one each.
- * Errors: BAD_ARG, TOO_LARGE, CUDA (the workspace's size: BAD_ARG as a negative number). */
+ * Errors: BAD_ARG, TOO_LARGE, CUDA (the workspace's size: BAD_ARG as a negative number).  The call is two launches: should the device refuse the second
+ * after the first (CUDA), what the first had to write is written all the same: the gradients of x, h and gate. */
 typedef struct {
     int64_t rows;
     int32_t cols;

@@ -24,6 +24,17 @@ struct DeviceGuard {
     DeviceGuard& operator=(const DeviceGuard&) = delete;
 };
 
+// Launch `kernel` the plain way; what the launch itself returns, and not the last error, which may be an earlier call's.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_plain(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args&&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
 // Launch `kernel` so that it may begin while the kernel before it in the stream is still running (programmatic
 // dependent launch): the kernel itself waits, by dependency_wait(), before it touches that kernel's results.
 template <typename... KArgs, typename... Args>

@@ -19,7 +19,12 @@ namespace {
 constexpr int kMostCols = 8192;               // of a norm
 constexpr int kMostDevices = 64;
 
-int status() { return cudaGetLastError() == cudaSuccess ? CUTOFF_OK : CUTOFF_ERR_CUDA; }
+// The result of a call whose CUDA calls all returned success, or not: the thread's last error, which whoever asks next would take for its own, ends here.
+int done(bool ok) {
+    if (ok) return CUTOFF_OK;
+    cudaGetLastError();
+    return CUTOFF_ERR_CUDA;
+}
 
 int sm_count(int device) {
     static int sms[kMostDevices] = {};
@@ -56,7 +61,7 @@ constexpr int kMostProductCols = 1 << 30;     // of dropout, quantised rows and 
 
 // ---- dropout ---------------------------------------------------------------------------------------------------------
 template <typename T, int V, int LX>
-void launch_dropout(const DropoutArgs& a, int sms, cudaStream_t s) {
+bool launch_dropout(const DropoutArgs& a, int sms, cudaStream_t s) {
     // rows of a thread on their way: as many as fit 80 registers
     constexpr int kAdd = sizeof(T) == 2 ? 3 : 2, kPlain = V == 1 ? kAdd : sizeof(T) == 2 ? 5 : 3, kWarps = kDropoutThreads / 32;
     const int unroll = a.residual ? kAdd : kPlain;
@@ -65,20 +70,20 @@ void launch_dropout(const DropoutArgs& a, int sms, cudaStream_t s) {
     int64_t each = resident / a.tiles;
     each = each < 1 ? 1 : each < row_warps ? each : row_warps;
     const unsigned grid = static_cast<unsigned>(ceil_div64(each * a.tiles, kWarps));
-    if (a.residual) k_dropout<T, V, LX, kAdd, true><<<grid, kDropoutThreads, 0, s>>>(a);
-    else k_dropout<T, V, LX, kPlain, false><<<grid, kDropoutThreads, 0, s>>>(a);
+    return launch_plain(a.residual ? k_dropout<T, V, LX, kAdd, true> : k_dropout<T, V, LX, kPlain, false>, dim3(grid), dim3(kDropoutThreads), 0, s, a) ==
+           cudaSuccess;
 }
 template <typename T, int V>
-void launch_dropout(DropoutArgs& a, int sms, cudaStream_t s) {
+bool launch_dropout(DropoutArgs& a, int sms, cudaStream_t s) {
     const int groups = ceil_div(a.cols, 8);
     const auto run = [&](auto lanes) {
         constexpr int LX = decltype(lanes)::value;
         a.tiles = ceil_div(groups, LX);
-        launch_dropout<T, V, LX>(a, sms, s);
+        return launch_dropout<T, V, LX>(a, sms, s);
     };
-    if (groups <= 2) run(std::integral_constant<int, 2>{});
-    else if (groups <= 8) run(std::integral_constant<int, 8>{});
-    else run(std::integral_constant<int, 32>{});
+    return groups <= 2   ? run(std::integral_constant<int, 2>{})
+           : groups <= 8 ? run(std::integral_constant<int, 8>{})
+                         : run(std::integral_constant<int, 32>{});
 }
 
 // ---- norms -----------------------------------------------------------------------------------------------------------
@@ -167,19 +172,15 @@ bool launch_product_pair(const ProductArgs& p, int device, cudaStream_t s) {
     if (cudaFuncSetAttribute(k_product_pair<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kPairSmem)) != cudaSuccess) return false;
     const int channel_tiles = ceil_div(p.n, 2 * kProdM), token_tiles = static_cast<int>(ceil_div64(p.m, kPairTokens)), pairs = sm_count(device) / 2;
     const int64_t tiles = static_cast<int64_t>(channel_tiles) * token_tiles;
-    launch_dependent(k_product_pair<T>, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), dim3(kPairThreads), kPairSmem, s, map_b, map_a, p,
-                     channel_tiles, token_tiles);
-    return true;
+    return launch_dependent(k_product_pair<T>, dim3(static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs))), dim3(kPairThreads), kPairSmem, s, map_b,
+                            map_a, p, channel_tiles, token_tiles) == cudaSuccess;
 }
 
 template <typename T>
 bool launch_product(const ProductArgs& p, int device, cudaStream_t s) {
     // One token: as its products are few, the vector unit's dot products follow the weights (4096 x 4096 6.1 us, tensor-core tiles 8.5; 8192 x 8192
     // 15.4 and 16.0); with two they do not any more (11.3, 8.5).
-    if (p.m == 1) {
-        launch_dependent(k_product_dot<T>, dim3(ceil_div(p.n, kDotWarps)), dim3(kDotWarps * 32), 0, s, p);
-        return true;
-    }
+    if (p.m == 1) return launch_dependent(k_product_dot<T>, dim3(ceil_div(p.n, kDotWarps)), dim3(kDotWarps * 32), 0, s, p) == cudaSuccess;
     // The fewest tokens per tile that hold them all, or whose tiles, split in four, are resident at a time: the latency of the K blocks bounds a CTA, and
     // what a second tile reads again comes from the L2 (300 x 512 x 8192: 32 tokens 12 us, 64 13, 128 21).  Then whole tiles of 128 tokens, one per
     // SM (512 x 4096 x 4096 16.3 us, pairs of SMs 17.9), then pairs (1000 x 4096 x 4096 18.0 us, tiles of 128 tokens 28.6).
@@ -203,7 +204,7 @@ int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const v
     if (cols > kMostProductCols) return CUTOFF_ERR_TOO_LARGE;
     if (rows == 0) return CUTOFF_OK;
     DeviceGuard guard(device);
-    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    if (guard.err != cudaSuccess) return done(false);
     const uint32_t dropped = static_cast<uint32_t>(std::nearbyint(p * 65536.0));
     DropoutArgs a{};
     a.x = x; a.residual = residual; a.y = y;
@@ -216,12 +217,13 @@ int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const v
     const int size = type_size(type);
     const bool packs = cols * static_cast<int64_t>(size) % 16 == 0 && rows_aligned(x, x_ld, size, 16) && rows_aligned(residual, residual_ld, size, 16) &&
                        rows_aligned(y, y_ld, size, 16);
+    bool ok = false;
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        if (packs) launch_dropout<T, kPack<T>>(a, sm_count(device), static_cast<cudaStream_t>(stream));
-        else launch_dropout<T, 1>(a, sm_count(device), static_cast<cudaStream_t>(stream));
+        ok = packs ? launch_dropout<T, kPack<T>>(a, sm_count(device), static_cast<cudaStream_t>(stream))
+                   : launch_dropout<T, 1>(a, sm_count(device), static_cast<cudaStream_t>(stream));
     });
-    return status();
+    return done(ok);
 }
 
 int cutoff_residual_norm(int device, const cutoff_norm_layer* layer, void* residual, int64_t residual_ld, void* norm, int64_t norm_ld, float* norm_scale,
@@ -232,7 +234,7 @@ int cutoff_residual_norm(int device, const cutoff_norm_layer* layer, void* resid
     if (layer->cols > kMostCols) return CUTOFF_ERR_TOO_LARGE;
     if (layer->rows == 0) return CUTOFF_OK;
     DeviceGuard guard(device);
-    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    if (guard.err != cudaSuccess) return done(false);
     NormArgs a = norm_args(layer);
     a.r = residual; a.n = norm; a.n_scale = norm_scale; a.r_ld = residual_ld; a.n_ld = norm_ld;
     const int size = type_size(layer->type);
@@ -240,7 +242,7 @@ int cutoff_residual_norm(int device, const cutoff_norm_layer* layer, void* resid
                        (norm_scale ? rows_aligned(norm, norm_ld, 1, 16 / size) : rows_aligned(norm, norm_ld, size, 16));
     bool ok = false;
     with_type(layer->type, [&](auto t) { ok = run_norm<decltype(t)>(a, packs, sm_count(device), static_cast<cudaStream_t>(stream)); });
-    return ok ? status() : CUTOFF_ERR_CUDA;
+    return done(ok);
 }
 
 int64_t cutoff_residual_norm_grad_workspace_bytes(int64_t rows, int32_t cols) {
@@ -270,7 +272,7 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
     if (static_cast<int64_t>(workspace_bytes) < cutoff_residual_norm_grad_workspace_bytes(layer->rows, layer->cols) || !aligned16(workspace))
         return CUTOFF_ERR_BAD_ARG;
     DeviceGuard guard(device);
-    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    if (guard.err != cudaSuccess) return done(false);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int sms = sm_count(device);
     const bool bias = layer->post_bias || layer->pre_bias, groups = layer->gate && layer->gate_rows > 1;
@@ -293,8 +295,7 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
     const int gate_blocks = groups && grads->gate && layer->rows > 0 ? plan.teams * ceil_div(layer->cols, kFinishColumns * kFinishSlices) : 0;
     bool ok = false;
     with_type(layer->type, [&](auto t) { ok = run_norm_grad<decltype(t)>(q, plan, packs, bias, groups, q.column_blocks + gate_blocks, s); });
-    if (!ok) return CUTOFF_ERR_CUDA;
-    return status();
+    return done(ok);
 }
 
 int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, int8_t* q, int64_t q_ld, float* scale,
@@ -305,9 +306,10 @@ int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, c
     if (cols > kMostProductCols) return CUTOFF_ERR_TOO_LARGE;
     if (rows == 0) return CUTOFF_OK;
     DeviceGuard guard(device);
-    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    if (guard.err != cudaSuccess) return done(false);
     const QuantizeArgs a{x, q, scale, rows, x_ld, q_ld, cols};
     const int size = type_size(type);
+    bool ok = false;
     with_type(type, [&](auto t) {
         using T = decltype(t);
         const bool packs = cols % kPack<T> == 0 && rows_aligned(x, x_ld, size, 16) && rows_aligned(q, q_ld, 1, kPack<T>);
@@ -315,18 +317,16 @@ int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, c
             constexpr int V = decltype(v)::value;
             const cudaStream_t s = static_cast<cudaStream_t>(stream);
             // rows that a warp holds in registers; otherwise a CTA whose threads hold four packs each, or with few rows (their latency is all there is) one
-            if (cols <= 32 * V * kQuantizeKeep && rows > sm_count(device)) {
-                launch_dependent(k_quantize_rows<T, V, 32>, dim3(static_cast<unsigned>(ceil_div64(rows, kQuantizeWarps))), dim3(kQuantizeWarps * 32), 0, s, a);
-                return;
-            }
+            if (cols <= 32 * V * kQuantizeKeep && rows > sm_count(device))
+                return launch_dependent(k_quantize_rows<T, V, 32>, dim3(static_cast<unsigned>(ceil_div64(rows, kQuantizeWarps))), dim3(kQuantizeWarps * 32), 0, s, a) ==
+                       cudaSuccess;
             int threads = ceil_div(ceil_div(cols, rows > 2 * sm_count(device) ? V * kQuantizeKeep : V), 32) * 32;
             threads = threads > 512 ? 512 : threads;
-            launch_dependent(k_quantize_rows<T, V, 0>, dim3(static_cast<unsigned>(rows)), dim3(threads), 0, s, a);
+            return launch_dependent(k_quantize_rows<T, V, 0>, dim3(static_cast<unsigned>(rows)), dim3(threads), 0, s, a) == cudaSuccess;
         };
-        if (packs) run(std::integral_constant<int, kPack<T>>{});
-        else run(std::integral_constant<int, 1>{});
+        ok = packs ? run(std::integral_constant<int, kPack<T>>{}) : run(std::integral_constant<int, 1>{});
     });
-    return status();
+    return done(ok);
 }
 
 int cutoff_quantized_product(int device, int64_t m, int32_t n, int32_t k, const int8_t* a, int64_t a_ld, const float* a_scale, const int8_t* b,
@@ -337,11 +337,11 @@ int cutoff_quantized_product(int device, int64_t m, int32_t n, int32_t k, const 
     if (k > CUTOFF_PRODUCT_MAX_K || n > kMostProductCols) return CUTOFF_ERR_TOO_LARGE;
     if (m == 0) return CUTOFF_OK;
     DeviceGuard guard(device);
-    if (guard.err != cudaSuccess) return CUTOFF_ERR_CUDA;
+    if (guard.err != cudaSuccess) return done(false);
     const ProductArgs p{a, b, a_scale, b_scale, bias, y, m, a_ld, b_ld, y_ld, n, k};
     bool ok = false;
     with_type(type, [&](auto t) { ok = launch_product<decltype(t)>(p, device, static_cast<cudaStream_t>(stream)); });
-    return ok ? status() : CUTOFF_ERR_CUDA;
+    return done(ok);
 }
 
 }  // extern "C"

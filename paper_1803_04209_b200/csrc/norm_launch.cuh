@@ -65,8 +65,7 @@ bool launch_norm(const NormArgs& a, int sms, cudaStream_t s) {
         if (ctas <= sms * st.per_sm) st.stages = 1, st.bytes = stage + gate;  // a row each
         ops.stages = st.stages;
         if (st.bytes > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, st.bytes) != cudaSuccess) return;
-        kernel<<<ctas < sms * st.per_sm ? ctas : sms * st.per_sm, threads, st.bytes, s>>>(a, ops, st.stages * stage);
-        ok = true;
+        ok = launch_plain(kernel, dim3(ctas < sms * st.per_sm ? ctas : sms * st.per_sm), dim3(threads), st.bytes, s, a, ops, st.stages * stage) == cudaSuccess;
     });
     return ok;
 }
@@ -112,8 +111,7 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
         const int sums = SIZE ? g.f.cols * 4 : 0;
         if (st.bytes < sums) st.bytes = sums;
         if (st.bytes > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, st.bytes) != cudaSuccess) return;
-        kernel<<<plan.ctas, plan.threads, st.bytes, s>>>(g, ops);
-        ok = true;
+        ok = launch_plain(kernel, dim3(plan.ctas), dim3(plan.threads), st.bytes, s, g, ops) == cudaSuccess;
     };
     using std::integral_constant;
     constexpr integral_constant<int, 8 / V> eight{};
@@ -145,8 +143,9 @@ bool run_norm_grad(NormFinishArgs& q, const GradPlan& plan, bool packs, bool bia
         if (packs) run(std::integral_constant<int, kPack<T>>{});
         else run(std::integral_constant<int, 1>{});
     }
-    if (ok && finish_blocks > 0) launch_dependent(k_norm_grad_finish<T>, dim3(finish_blocks), dim3(kFinishColumns * kFinishSlices), 0, s, q);
-    return ok;
+    // sums that no kernel has formed are not added up
+    if (!ok || finish_blocks == 0) return ok;
+    return launch_dependent(k_norm_grad_finish<T>, dim3(finish_blocks), dim3(kFinishColumns * kFinishSlices), 0, s, q) == cudaSuccess;
 }
 
 }  // namespace layers
