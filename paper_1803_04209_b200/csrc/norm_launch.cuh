@@ -27,15 +27,26 @@ inline int team_threads(int cols, int per_thread) { return ceil_div(ceil_div(col
 // Most bytes of shared memory that the CTAs of an SM may take together for their operands.
 constexpr int kNormSmem = 228 * 1024;
 
+constexpr int kNormFixed = 2560;                  // what the system and static arrays take of a CTA, at most
+// Most dynamic shared memory that any of these kernels is ever given (rows of 8192 fp32 values take 225 KB of it).
+constexpr int kNormDynamic = kNormSmem - kNormFixed;
+
+// Allows a kernel what it may ever need.  The limit belongs to the kernel on the device, whichever host thread sets it: a call that set its own size would
+// lower it between another thread's setting and launch.
+template <typename Kernel>
+bool allow_smem(Kernel kernel, int bytes) {
+    if (bytes <= 40 * 1024) return true;          // with static arrays, what every kernel may have
+    return bytes <= kNormDynamic && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormDynamic) == cudaSuccess;
+}
+
 // CTAs of an SM and rows of a team in shared memory: `most` CTAs by their registers; two stages unless they do not fit even one CTA.
 struct Staging {
     int per_sm, stages, bytes;
 };
 inline Staging staging(int most, int stage_bytes, int more_bytes) {
-    constexpr int kFixed = 2560;                  // what the system and static arrays take of a CTA, at most
     Staging s{most, 2, 0};
-    while (s.per_sm > 1 && s.per_sm * (2 * stage_bytes + more_bytes + kFixed) > kNormSmem) --s.per_sm;
-    if (2 * stage_bytes + more_bytes + kFixed > kNormSmem) s.stages = 1;
+    while (s.per_sm > 1 && s.per_sm * (2 * stage_bytes + more_bytes + kNormFixed) > kNormSmem) --s.per_sm;
+    if (2 * stage_bytes + more_bytes + kNormFixed > kNormSmem) s.stages = 1;
     s.bytes = s.stages * stage_bytes + more_bytes;
     return s;
 }
@@ -64,7 +75,7 @@ bool launch_norm(const NormArgs& a, int sms, cudaStream_t s) {
         Staging st = staging(most, stage, gate);
         if (ctas <= sms * st.per_sm) st.stages = 1, st.bytes = stage + gate;  // a row each
         ops.stages = st.stages;
-        if (st.bytes > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, st.bytes) != cudaSuccess) return;
+        if (!allow_smem(kernel, st.bytes)) return;
         ok = launch_plain(kernel, dim3(ctas < sms * st.per_sm ? ctas : sms * st.per_sm), dim3(threads), st.bytes, s, a, ops, st.stages * stage) == cudaSuccess;
     });
     return ok;
@@ -110,7 +121,7 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
         g.param_bytes = st.stages * stage + gate;
         const int sums = SIZE ? g.f.cols * 4 : 0;
         if (st.bytes < sums) st.bytes = sums;
-        if (st.bytes > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, st.bytes) != cudaSuccess) return;
+        if (!allow_smem(kernel, st.bytes)) return;
         ok = launch_plain(kernel, dim3(plan.ctas), dim3(plan.threads), st.bytes, s, g, ops) == cudaSuccess;
     };
     using std::integral_constant;

@@ -134,3 +134,36 @@ def _in_threads(rounds=4000):
 def test_a_call_that_fails_has_written_no_sums():
     failed, written = _in_threads()
     assert not written, (len(failed), len(written))
+
+
+def test_threads_with_rows_of_several_widths_do_not_fail_one_another():
+    failed, _ = _in_threads()
+    assert not failed, len(failed)
+
+
+def _forward_calls(cols, rounds, failed, barrier):
+    lib = binding.load_library()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        x = torch.randn(2000, cols, device="cuda")
+        n = torch.empty_like(x)
+        layer = binding.NormLayer(2000, cols, binding.TYPE_FP32, x.data_ptr(), cols, x.data_ptr(), cols, None, 0, 1, 0, 1, 1, 1e-6)
+        stream.synchronize()
+        barrier.wait()
+        for i in range(rounds):
+            if i % 64 == 0:
+                stream.synchronize()
+            rc = lib.cutoff_residual_norm(0, C.byref(layer), None, 0, n.data_ptr(), cols, None, stream.cuda_stream)
+            if rc != binding.OK:
+                failed.append(rc)
+        stream.synchronize()
+
+
+def test_threads_with_norms_of_several_widths_do_not_fail_one_another():
+    failed, barrier = [], threading.Barrier(4)
+    threads = [threading.Thread(target=_forward_calls, args=(cols, 4000, failed, barrier)) for cols in (8192, 6144, 8192, 5120)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, len(failed)
