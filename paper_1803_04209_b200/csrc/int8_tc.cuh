@@ -308,9 +308,7 @@ k_product_pair(const __grid_constant__ CUtensorMap map_b, const __grid_constant_
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))), "r"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        tc::tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
     }
     tc::tc_fence_before();
     __syncthreads();
@@ -448,7 +446,7 @@ k_product_pair(const __grid_constant__ CUtensorMap map_b, const __grid_constant_
     tc::cluster_sync_all();               // neither CTA frees its tensor memory or leaves while the other may still reach it
     if (warp == 1) {
         tc::tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+        tc::tmem_free_pair(tmem, 512);
     }
 }
 

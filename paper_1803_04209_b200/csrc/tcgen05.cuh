@@ -90,5 +90,15 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint16_t cta_mask
                  ::"r"(bar), "h"(cta_mask) : "memory");
 }
 
+// Tensor memory of a pair of SMs: a kernel whose products span two SMs names cta_group::2 in all its tcgen05 instructions.  One warp of either CTA calls
+// these, both CTAs being there; the address that each finds in its own slot is the same in both.
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t slot, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free_pair(uint32_t tmem, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+}
+
 }  // namespace tc
 }  // namespace cutoff

@@ -21,3 +21,21 @@ def test_lanes_meet_before_a_barrier_that_takes_whole_warps(name):
     for m in found:
         before = source[: m.start()].rstrip()
         assert before.endswith("__syncwarp();"), source[m.start(): m.end()]
+
+
+def _body(source: str, kernel: str) -> str:
+    at = source.index("{", source.index(kernel + "("))
+    depth, i = 1, at + 1
+    while depth:
+        depth += {"{": 1, "}": -1}.get(source[i], 0)
+        i += 1
+    return source[at: i]
+
+
+# All tcgen05 instructions of a kernel have one group size: those of the kernels on pairs of SMs have two, their tensor memory included.
+@pytest.mark.parametrize("name,kernel", [("int8_tc.cuh", "k_product_pair"), ("emit_tc2.cuh", "k_emit_tc2")])
+def test_kernels_on_pairs_name_one_group_size(name, kernel):
+    body = _body(_source(name), kernel)
+    assert "cta_group::1" not in body and "umma_commit(" not in body and "umma_s8(" not in body
+    for helper in ("tmem_alloc_pair", "tmem_free_pair", "umma_commit_pair"):
+        assert helper in body and "cta_group::1" not in _body(_source("tcgen05.cuh"), "void " + helper)
