@@ -383,7 +383,8 @@ int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const v
  *     r = x + scale * act(gate) * post(h)          n = pre(r)
  * where post and pre are CUTOFF_NORM_*: RMS v / sqrt(mean(v^2) + eps), LAYER (v - mean(v)) / sqrt(var(v) + eps) (population variance), times the weight
  * plus the bias (NULL: ones, zeros), or NONE, which still applies weight and bias.  gate is a row for every gate_rows rows of x (1: one for each
- * row; the last group may be shorter); act is CUTOFF_GATE_*: g, 1 / (1 + exp(-g)), g / (1 + exp(-g)).  NULL: gate 1, scale 1.  With h NULL
+ * row; the last group may be shorter); act is CUTOFF_GATE_*: g, 1 / (1 + exp(-g)), g / (1 + exp(-g)).  fp32: act within 6 units of the last place for any
+ * gate; 16-bit types: act within (2 |g| + 11) 2^-24 of itself before the result is rounded, zero where the sigmoid is below 2^-126.  NULL: gate 1, scale 1.  With h NULL
  * there is no block: r = x (scale, gate, post_weight and post_bias must be NULL).  rows <= 2^30, cols <= 8192 (TOO_LARGE otherwise), eps > 0.
  *
  * cutoff_residual_norm: residual (rows x cols, receives r; NULL = not wanted; must be NULL without h) and norm (receives n; NULL = not wanted).

@@ -42,27 +42,48 @@ struct NormArgs {
     int64_t r_ld, n_ld;
 };
 
-// 1 / (1 + exp(-g)); exp of a large -g is infinite and the result 0.  Within some units of the last place for gates of ordinary size.
-__device__ __forceinline__ float logistic(float g) {
-    float e, s;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
-    return s;
+// 1 / (1 + exp(-g)) and, with SLOPE, its derivative, both from u = exp(-|g|) <= 1 and s = 1 / (1 + u): the value is s or u s, and the derivative u s s and
+// not a difference value - value^2, of which nothing is left where the value is close to 1.  fp32: u to two units of the last place, value within six and
+// derivative within eight of them, whatever the gate.  What is rounded to 16 bits takes the hardware's exponential of |g| log2(e), a few instructions
+// less for each value: within 2 |g| + 10 units of 2^-24, a hundredth of its own rounding, and zero below 2^-126.
+template <typename T, bool SLOPE>
+__device__ __forceinline__ float logistic(float g, float& slope) {
+    float u, s;
+    if constexpr (sizeof(T) == 4) u = expf(-fabsf(g));
+    else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(u) : "f"(fabsf(g) * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + u));
+    const float small = u * s;
+    if constexpr (SLOPE) slope = small * s;
+    return g < 0.f ? small : s;
 }
-// g becomes act(g), and with SLOPE slope its derivative.
-template <int KIND, bool SLOPE, typename N, int M>
+template <typename T, bool SLOPE>
+__device__ __forceinline__ F1 logistic(F1 g, F1& slope) { return F1{logistic<T, SLOPE>(g.v, slope.v)}; }
+template <typename T, bool SLOPE>
+__device__ __forceinline__ F2 logistic(F2 g, F2& slope) {
+    float x, y, s = 0.f, t = 0.f;
+    unpack2(g.v, x, y);
+    x = logistic<T, SLOPE>(x, s);
+    y = logistic<T, SLOPE>(y, t);
+    if constexpr (SLOPE) slope.v = pack2(s, t);
+    return F2{pack2(x, y)};
+}
+// g, a gate of type T, becomes act(g), and with SLOPE slope its derivative.
+template <typename T, int KIND, bool SLOPE, typename N, int M>
 __device__ __forceinline__ void gate_values(N (&g)[M], N (&slope)[M]) {
 #pragma unroll
     for (int i = 0; i < M; ++i) {
         if constexpr (KIND == kGateLinear) {
             if constexpr (SLOPE) slope[i] = splat<N>(1.f);
-        } else if constexpr (KIND == kGateSigmoid) {
-            g[i] = each(g[i], logistic);
-            if constexpr (SLOPE) slope[i] = fma(mul(g[i], splat<N>(-1.f)), g[i], g[i]);
         } else {
-            const N t = each(g[i], logistic);
-            g[i] = mul(g[i], t);
-            if constexpr (SLOPE) slope[i] = fma(g[i], fma(t, splat<N>(-1.f), splat<N>(1.f)), t);
+            N d;
+            const N s = logistic<T, SLOPE>(g[i], d);
+            if constexpr (KIND == kGateSigmoid) {
+                g[i] = s;
+                if constexpr (SLOPE) slope[i] = d;
+            } else {
+                if constexpr (SLOPE) slope[i] = fma(g[i], d, s);
+                g[i] = mul(g[i], s);
+            }
         }
     }
 }
@@ -265,7 +286,7 @@ struct GroupGate {
         with_gate(a.gate_kind, [&](auto kind) {
             put([&](int k, Num<V> (&u)[kNums<V>]) {
                 read_global<T, V>(row + (col.has(k) ? col(k) : 0), u);
-                gate_values<decltype(kind)::value, false>(u, u);
+                gate_values<T, decltype(kind)::value, false>(u, u);
                 if (!col.has(k))
 #pragma unroll
                     for (int i = 0; i < kNums<V>; ++i) u[i] = splat<Num<V>>(0.f);
@@ -366,7 +387,7 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormAr
                     for (int k = 0; k < K; ++k) {
                         N t[M];
                         take<T, V>(gate_at, col, k, columns, t);
-                        gate_values<decltype(kind)::value, false>(t, t);
+                        gate_values<T, decltype(kind)::value, false>(t, t);
                         add_x(k, t);
                     }
                 });
@@ -562,7 +583,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
                         for (int k = 0; k < K; ++k) {
                             N t[M];
                             take<T, V>(gate_at, col, k, columns, t);
-                            gate_values<decltype(kind)::value, false>(t, t);
+                            gate_values<T, decltype(kind)::value, false>(t, t);
                             add_x(k, t);
                         }
                     });
@@ -660,7 +681,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
                         N w[M], u[M], slope[M], p[M];
                         param_of(0, k, w);
                         take<T, V>(gate_at, col, k, columns, u);
-                        gate_values<decltype(kind)::value, true>(u, slope);
+                        gate_values<T, decltype(kind)::value, true>(u, slope);
                         branch_of(k, w, p);
 #pragma unroll
                         for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], mul(d[k][i], p[i]));
@@ -703,7 +724,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
                             if (whole) {
                                 N u[M], slope[M];
                                 read_global<T, V>(static_cast<const T*>(a.gate) + group * a.gate_ld + col(k), u);
-                                with_gate(a.gate_kind, [&](auto kind) { gate_values<decltype(kind)::value, true>(u, slope); });
+                                with_gate(a.gate_kind, [&](auto kind) { gate_values<T, decltype(kind)::value, true>(u, slope); });
 #pragma unroll
                                 for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], gate_sum[k][i]);
                                 if (g.d_gate) write_global<T, V>(static_cast<T*>(g.d_gate) + group * g.d_gate_ld, col(k), a.cols, slope);
@@ -780,7 +801,7 @@ __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_fi
 #pragma unroll 8                                   // loads that wait for nothing
         for (int v = t + 1; v < stop; ++v) s += q.g.gate_sums[2 * static_cast<int64_t>(v) * a.cols + c];
         F1 u[1] = {F1{to_float(static_cast<const T*>(a.gate)[group * a.gate_ld + c])}}, slope[1];
-        with_gate(a.gate_kind, [&](auto kind) { gate_values<decltype(kind)::value, true>(u, slope); });
+        with_gate(a.gate_kind, [&](auto kind) { gate_values<T, decltype(kind)::value, true>(u, slope); });
         from_float(static_cast<T*>(q.g.d_gate)[group * q.g.d_gate_ld + c], s * slope[0].v);
         return;
     }

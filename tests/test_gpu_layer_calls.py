@@ -1,5 +1,5 @@
 """The layer operators in calls that their users may make and that values alone do not cover: warps of which some lanes have no work, launches that the
-runtime refuses, several host threads."""
+runtime refuses, several host threads; gates far from zero."""
 import ctypes as C
 import threading
 
@@ -8,6 +8,7 @@ import pytest
 import torch
 
 from paper_1803_04209_b200 import binding, build
+from layer_tools import TYPES, U, close, host, rounding
 
 pytestmark = pytest.mark.gpu
 
@@ -167,3 +168,65 @@ def test_threads_with_norms_of_several_widths_do_not_fail_one_another():
     for t in threads:
         t.join()
     assert not failed, len(failed)
+
+
+# ---- gates far from zero ---------------------------------------------------------------------------------------------------------
+def _gates(dtype, cols):
+    """Gates of all sizes, the ends among them, as rows; and their values in 64 bits."""
+    rng = np.random.default_rng(cols)
+    g = np.concatenate([np.linspace(-110, 110, 2201), rng.standard_normal(2000) * 5, 10.0 ** rng.uniform(-30, 0, 500), -(10.0 ** rng.uniform(-30, 0, 500)),
+                        [0.0, -0.0, 87.0, -87.0, 88.5, -88.5, 104.0, -104.0, 1e4, -1e4, np.inf, -np.inf, np.nan]])
+    g = torch.from_numpy(np.resize(g, (-(-len(g) // cols), cols))).to(TYPES[dtype]).cuda()
+    return g, host(g)
+
+
+def _logistic(g):
+    """Value and derivative of the sigmoid in 64 bits, neither of them a difference of neighbours."""
+    u = np.exp(-np.abs(g))
+    value = np.where(np.isnan(g), np.nan, np.where(g < 0, u / (1 + u), 1 / (1 + u)))
+    return value, u / (1 + u) ** 2
+
+
+def _gate_bounds(g, dtype):
+    """How far value and derivative of the sigmoid may be off, relative to themselves, and absolutely.
+
+    fp32: exp(-|g|) is off by 2 steps = 4 U; 1 + it is rounded (U), its reciprocal 1 step = 2 U off: 5 U with half of the exponential's error; their product is
+    4 + 5 + 1 = 10 U off, and once more times the reciprocal 16 U.  16 bits: the exponent |g| log2(e) is rounded twice, by U each, which the exponential
+    multiplies by |g|; results below 2^-126 may be 0."""
+    if dtype == "fp32":
+        return 10 * U, 16 * U, 2.0 ** -148
+    steps = 2 * np.minimum(np.abs(np.nan_to_num(g, nan=0.0, posinf=200.0, neginf=-200.0)), 200.0) * U
+    return 10 * U + steps, 16 * U + steps, 2.0 ** -126
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("kind", ["sigmoid", "silu"])
+@pytest.mark.parametrize("cols,gate_rows", [(24, 1), (25, 1), (512, 1), (1024, 1), (1001, 1), (1024, 2), (1001, 3), (40, 5)])
+def test_gates_of_any_size(dtype, kind, cols, gate_rows):
+    gate, g = _gates(dtype, cols)
+    rows = len(g) * gate_rows
+    x, h = torch.zeros(rows, cols, device="cuda", dtype=gate.dtype), torch.ones(rows, cols, device="cuda", dtype=gate.dtype)
+    kw = dict(gate=gate, gate_rows=gate_rows, gate_kind=kind, post=None, pre=None)
+    r, _ = binding.residual_norm(x, h, want_norm=False, **kw)                    # 0 + act(gate) * 1
+    grads = binding.residual_norm_grad(x, h, h, None, **kw)                      # the gate's: the derivative, gate_rows times
+    with np.errstate(invalid="ignore"):
+        value, slope = _logistic(g)
+        value_off, slope_off, least = _gate_bounds(g, dtype)
+        value_off, slope_off = value_off * value, slope_off * slope
+        if kind == "silu":
+            value, slope, value_off, slope_off = g * value, value + g * slope, np.abs(g) * (value_off + U * value), value_off + np.abs(g) * (slope_off + U * slope)
+            slope_off = slope_off + U * np.abs(slope)
+            least = least * np.maximum(1, np.abs(g))
+    value_off, slope_off = (np.where(np.isfinite(off), off, 0) for off in (value_off + least, slope_off + least))      # what is not finite is compared exactly
+    each, bound = np.repeat(value, gate_rows, 0), np.repeat(value_off, gate_rows, 0)
+    finite = np.isfinite(each)
+    got = host(r)
+    assert np.array_equal(got[~finite], each[~finite], equal_nan=True)           # infinities and NaN as the formula has them
+    close(r.masked_fill(torch.from_numpy(~finite).cuda(), 0), np.where(finite, each, 0), bound + rounding(np.where(finite, each, 0), gate.dtype) * 1.001, "value")
+    close(grads["h"].masked_fill(torch.from_numpy(~finite).cuda(), 0), np.where(finite, each, 0), bound + rounding(np.where(finite, each, 0), gate.dtype) * 1.001, "h")
+    total = slope * gate_rows
+    finite = np.isfinite(total)
+    assert np.array_equal(host(grads["gate"])[~finite], total[~finite], equal_nan=True)
+    total = np.where(finite, total, 0)
+    bound = gate_rows * slope_off + gate_rows * U * np.abs(total) + rounding(total, gate.dtype) * 1.001
+    close(grads["gate"].masked_fill(torch.from_numpy(~finite).cuda(), 0), total, bound, "gate")
