@@ -542,7 +542,8 @@ class Fitter:
 
 # ---- layers of wider networks ----------------------------------------------------------------------------------------
 # Matrices are two-dimensional CUDA tensors (fp32, fp16 or bf16) whose rows are contiguous; rows may be further apart than they are long.
-# Parameters are contiguous fp32 vectors.  Work goes to torch's current stream of the tensors' device.
+# Parameters are contiguous fp32 vectors.  Work goes to torch's current stream of the tensors' device.  Autograd does not see these calls: tensors that
+# require a gradient are refused unless gradients are off (torch.no_grad(), or detach()); what training needs is residual_norm_grad and dropout again.
 
 class Quantized(NamedTuple):
     """Rows of 8-bit integers and the scale of each row: value = integer * scale."""
@@ -576,8 +577,21 @@ def _type_of(dtype) -> int:
     return code
 
 
+def _no_gradient(t, what: str) -> None:
+    if t.requires_grad and _torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, which autograd would not get through this call: give it detached, or under torch.no_grad()")
+
+
+def _written(*results) -> None:
+    """Tells autograd that these tensors (or None) of the caller's have other values now."""
+    for t in results:
+        if t is not None and not t.is_inference():
+            _torch.autograd.graph.increment_version(t)
+
+
 def _matrix(t, what: str):
     """(address, leading dimension, rows, columns, device, type) of a CUDA matrix with contiguous rows."""
+    _no_gradient(t, what)
     shape, device = t.shape, t.get_device()
     if len(shape) != 2 or device < 0 or shape[1] < 1:
         raise ValueError(f"{what}: expected a CUDA matrix [rows, columns]")
@@ -614,6 +628,7 @@ def _result(x, out, what: str, rows: int, cols: int, device: int, dtype):
 def _vector(t, what: str, n: int, device: int) -> int:
     if t is None:
         return 0
+    _no_gradient(t, what)
     if t.dtype is not _torch.float32 or t.get_device() != device or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous fp32 vector of {n} values on cuda:{device}")
     return t.data_ptr() or 16
@@ -634,12 +649,14 @@ def dropout(x, p: float, seed: int, step: int = 0, noise_stream: int = STREAM_DR
     xp, x_ld, rows, cols, device, dtype = _matrix(x, "x")
     code = _type_of(dtype)
     rp, r_ld = _same(residual, "residual", rows, cols, device, dtype)
+    given = out
     out, op, o_ld = _result(x, out, "out", rows, cols, device, dtype)
     if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= noise_stream < 1 << 32):
         raise ValueError("seed has 64 bits, step and noise_stream 32")
     rc = lib.cutoff_dropout(device, code, rows, cols, xp, x_ld, rp, r_ld, op, o_ld, p, seed, step, noise_stream, first_row, _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_dropout")
+    _written(given)
     return out
 
 
@@ -680,6 +697,7 @@ def residual_norm(x, h=None, gate=None, gate_rows: int = 1, gate_kind: str = "li
     rc = lib.cutoff_residual_norm(device, layer, rp, r_ld, np_, n_ld, sp, _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_residual_norm")
+    _written(residual_out, norm_out)
     return r, n
 
 
@@ -738,6 +756,7 @@ def quantized_product(a, b, bias=None, dtype=None, out=None):
     if kind is not torch.int8:
         raise ValueError("expected rows of int8 values")
     n = bv.shape[0]
+    given = out
     bp, b_ld = _same(bv, "b", n, k, device, kind)
     if out is None:
         code = _type_of(dtype or torch.bfloat16)
@@ -750,6 +769,7 @@ def quantized_product(a, b, bias=None, dtype=None, out=None):
                                       _vector(b_scale, "b's scale", n, device), _vector(bias, "bias", n, device), code, op, o_ld, _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_quantized_product")
+    _written(given)
     return out
 
 

@@ -1,5 +1,5 @@
 """The layer operators in calls that their users may make and that values alone do not cover: warps of which some lanes have no work, launches that the
-runtime refuses, several host threads; gates far from zero."""
+runtime refuses, several host threads, tensors that autograd knows; gates far from zero."""
 import ctypes as C
 import threading
 
@@ -230,3 +230,41 @@ def test_gates_of_any_size(dtype, kind, cols, gate_rows):
     total = np.where(finite, total, 0)
     bound = gate_rows * slope_off + gate_rows * U * np.abs(total) + rounding(total, gate.dtype) * 1.001
     close(grads["gate"].masked_fill(torch.from_numpy(~finite).cuda(), 0), total, bound, "gate")
+
+
+# ---- tensors that autograd knows ---------------------------------------------------------------------------------------------------
+def test_tensors_that_require_a_gradient_are_refused_and_taken_without_one():
+    x = torch.randn(6, 64, device="cuda")
+    leaf, w, q = x.clone().requires_grad_(), torch.ones(64, device="cuda").requires_grad_(), binding.quantize_rows(x)
+    calls = [lambda t, w: binding.dropout(t, 0.5, 1), lambda t, w: binding.dropout(x, 0.5, 1, residual=t), lambda t, w: binding.residual_norm(t),
+             lambda t, w: binding.residual_norm(x, t), lambda t, w: binding.residual_norm(x, x, gate=t), lambda t, w: binding.residual_norm(x, x, scale=w),
+             lambda t, w: binding.residual_norm(x, pre_weight=w), lambda t, w: binding.residual_norm_grad(x, x, t, x),
+             lambda t, w: binding.residual_norm_grad(x, x, x, x, post_bias=w), lambda t, w: binding.quantize_rows(t),
+             lambda t, w: binding.quantized_product(q, q, bias=w[:6], dtype=torch.float32)]
+    flat = lambda r: list(r.values()) if isinstance(r, dict) else list(r) if isinstance(r, tuple) else [r]
+    for i, call in enumerate(calls):
+        for t, v in ((leaf, w), (leaf * 1.0, w * 1.0)):
+            with pytest.raises(ValueError, match="requires a gradient"):
+                call(t, v)
+        want = flat(call(x, w.detach()))
+        with torch.no_grad():
+            got = flat(call(leaf, w))
+        with torch.inference_mode():
+            inferred = flat(call(x, w))
+        assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(want, got, inferred)), i
+
+
+def test_autograd_learns_of_results_written_over_what_it_keeps():
+    x = torch.randn(6, 64, device="cuda")
+    writes = [lambda t: binding.dropout(x, 0.5, 1, out=t), lambda t: binding.residual_norm(x, x, residual_out=t), lambda t: binding.residual_norm(x, x, norm_out=t),
+              lambda t: binding.quantized_product(binding.quantize_rows(x), binding.quantize_rows(torch.ones(64, 64, device="cuda")), out=t)]
+    for write in writes:
+        leaf = x.clone().requires_grad_()
+        kept = leaf.exp()                                    # whose gradient needs it as it is
+        write(kept.detach())
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            kept.sum().backward()
+    with torch.inference_mode():
+        out = torch.empty_like(x)
+        binding.dropout(x, 0.5, 1, out=out)
+    assert torch.equal(out, binding.dropout(x, 0.5, 1))
