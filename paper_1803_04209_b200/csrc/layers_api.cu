@@ -251,7 +251,7 @@ int64_t cutoff_residual_norm_grad_workspace_bytes(int64_t rows, int32_t cols) {
     int64_t most = 0;
     for (const int way : {0, 1, 2}) {
         const GradPlan plan = grad_plan(static_cast<int>(rows), cols, way == 2 ? 4 : 2, way == 1, kMostSms);
-        const int64_t floats = (4 * static_cast<int64_t>(plan.ctas) + 2 * static_cast<int64_t>(plan.teams)) * cols;
+        const int64_t floats = 6 * static_cast<int64_t>(plan.ctas) * cols;
         most = floats > most ? floats : most;
     }
     return most * static_cast<int64_t>(sizeof(float)) + 256;
@@ -292,7 +292,16 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
                        rows_aligned(grads->gate, grads->gate_ld, size, 16);
     const bool sums = grads->scale || grads->post_weight || grads->post_bias || grads->pre_weight || grads->pre_bias;
     q.column_blocks = sums ? ceil_div(layer->cols, kFinishColumns) : 0;
-    const int gate_blocks = groups && grads->gate && layer->rows > 0 ? plan.teams * ceil_div(layer->cols, kFinishColumns * kFinishSlices) : 0;
+    int64_t gate_blocks = 0;
+    if (groups && grads->gate && layer->rows > 0) {
+        // a slice for every eight CTAs that a group may span
+        const int64_t cta_rows = static_cast<int64_t>(g.f.rows / plan.teams) * plan.per_cta, spans = g.f.gate_rows / (cta_rows > 0 ? cta_rows : 1) + 2;
+        q.teams_here = plan.per_cta;
+        q.groups = ceil_div64(g.f.rows, g.f.gate_rows);
+        q.slices = 1;
+        while (q.slices < kGateSlices && 8 * q.slices < spans && 8 * q.slices < plan.ctas) q.slices *= 2;
+        gate_blocks = static_cast<int64_t>(q.groups < plan.ctas ? q.groups : plan.ctas) * ceil_div(g.f.cols, kFinishThreads / q.slices);
+    }
     bool ok = false;
     with_type(layer->type, [&](auto t) { ok = run_norm_grad<decltype(t)>(q, plan, packs, bias, groups, q.column_blocks + gate_blocks, s); });
     return done(ok);

@@ -99,9 +99,9 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
         ops.row_bytes = g.f.cols * kSize;
         ops.slot_bytes = slot_bytes_of(ops.row_bytes, SIZE ? SIZE : plan.threads, V * K, kSize, V > 1);
         const int stage = kTeamsHere<SIZE> * ops.n * ops.slot_bytes,
-                  columns = (SIZE ? SIZE : plan.threads) * V * K, params = (BIAS ? 3 : 2) * 4 * columns, gate = GROUPS ? kTeamsHere<SIZE> * 4 * columns : 0;
+                  columns = (SIZE ? SIZE : plan.threads) * V * K, params = (BIAS ? 3 : 2) * 4 * columns, gate = GROUPS ? kTeamsHere<SIZE> * 4 * columns : 0, parts = SIZE ? 2 * gate : 0;
         // the plan's CTAs are resident by their registers; where shared memory holds fewer, the others follow
-        Staging st = staging(plan.per_sm, stage, params + gate);
+        Staging st = staging(plan.per_sm, stage, params + gate + parts);
         const bool layer = g.f.post == kNormLayer || g.f.pre == kNormLayer;
         // 168 registers where they are needed and the row's threads leave them
         constexpr int kThreads = V * K == 16 && (BIAS || GROUPS) ? kGradThreadsMany : kGradThreads;
@@ -119,6 +119,7 @@ bool launch_grad(NormFinishArgs& q, const GradPlan& plan, cudaStream_t s) {
         ops.stages = st.stages;
         g.gate_bytes = st.stages * stage;
         g.param_bytes = st.stages * stage + gate;
+        g.part_bytes = st.stages * stage + gate + params;
         const int sums = SIZE ? g.f.cols * 4 : 0;
         if (st.bytes < sums) st.bytes = sums;
         if (!allow_smem(kernel, st.bytes)) return;
@@ -141,7 +142,7 @@ template <typename T>
 bool run_norm(const NormArgs& a, bool packs, int sms, cudaStream_t s) { return packs ? launch_norm<T, kPack<T>>(a, sms, s) : launch_norm<T, 1>(a, sms, s); }
 
 template <typename T>
-bool run_norm_grad(NormFinishArgs& q, const GradPlan& plan, bool packs, bool bias, bool groups, int finish_blocks, cudaStream_t s) {
+bool run_norm_grad(NormFinishArgs& q, const GradPlan& plan, bool packs, bool bias, bool groups, int64_t finish_blocks, cudaStream_t s) {
     bool ok = true;
     const auto run = [&](auto v) {
         constexpr int V = decltype(v)::value;
@@ -156,7 +157,7 @@ bool run_norm_grad(NormFinishArgs& q, const GradPlan& plan, bool packs, bool bia
     }
     // sums that no kernel has formed are not added up
     if (!ok || finish_blocks == 0) return ok;
-    return launch_dependent(k_norm_grad_finish<T>, dim3(finish_blocks), dim3(kFinishColumns * kFinishSlices), 0, s, q) == cudaSuccess;
+    return launch_dependent(k_norm_grad_finish<T>, dim3(static_cast<unsigned>(finish_blocks)), dim3(kFinishThreads), 0, s, q) == cudaSuccess;
 }
 
 }  // namespace layers

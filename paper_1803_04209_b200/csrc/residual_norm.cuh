@@ -297,6 +297,11 @@ struct GroupGate {
 };
 // Rows of team t where the teams' rows are consecutive.
 __device__ __forceinline__ int first_row_of(int t, int teams, int rows) { return rows / teams * t + min(t, rows % teams); }
+// The team that has a row.
+__device__ __forceinline__ int team_of(int row, int teams, int rows) {
+    const int each = rows / teams, more = rows % teams;        // the first `more` teams have a row more
+    return row < more * (each + 1) ? row / (each + 1) : more + (row - more * (each + 1)) / each;
+}
 // Rows of a team.  With groups of rows they are consecutive, so that a group's gate and its gradient stay with few teams; otherwise the teams take
 // turns, so that what is read and written at a time lies together (16384 rows of 4096 bf16 values with gate: 106 us, consecutive rows 150).
 template <bool GROUPS>
@@ -450,16 +455,61 @@ struct NormGradArgs {
     void *d_x, *d_h, *d_gate;                     // each may be null
     int64_t d_x_ld, d_h_ld, d_gate_ld;
     float* sums;                                  // [CTAs][2 or 4][cols]: sum e * hat, sum d_n * r_hat, with BIAS also sum e, sum d_n
-    float* gate_sums;                             // [teams][2][cols]: of the team's first and last group, where another team has the rest
+    float* gate_sums;                             // [CTAs][2][cols]: of the CTA's first and last group, where another CTA has the rest
     int teams;
     int gate_bytes;                               // offset in shared memory of the teams' group gates
     int param_bytes;                              // offset in shared memory of the parameters: scale * post_w, pre_w, with BIAS scale * post_b
+    int part_bytes;                               // offset in shared memory of [teams here][2][columns of a team's threads]: as gate_sums, of warp teams
 };
 constexpr int kGradThreads = 512;                 // most threads of a CTA: 128 registers each
 constexpr int kGradThreadsMany = 384;             // with 16 values and many sums: 168, where the row allows it
 // CTAs of warp teams per SM: 128 registers for each thread, 168 with 16 values and many sums.
 template <int VALUES, bool MORE>
 constexpr int kGradWarpCtas = VALUES > 8 && MORE ? 3 : 4;
+
+// Of a group of rows and a range of them: the group of a row, where it starts and ends.
+struct Group {
+    int64_t start, end;
+    int at;
+    __device__ __forceinline__ Group(int row, const NormArgs& a)
+        : start(static_cast<int64_t>(row / a.gate_rows) * a.gate_rows), end(min(start + a.gate_rows, static_cast<int64_t>(a.rows))), at(row / a.gate_rows) {}
+};
+// The gradient of a group's gate in column c, given the sum over the group's rows.
+template <typename T>
+__device__ __forceinline__ void finish_gate(const NormGradArgs& g, int group, int c, float sum) {
+    const NormArgs& a = g.f;
+    F1 u[1] = {F1{to_float(static_cast<const T*>(a.gate)[group * a.gate_ld + c])}}, slope[1];
+    with_gate(a.gate_kind, [&](auto kind) { gate_values<T, decltype(kind)::value, true>(u, slope); });
+    from_float(static_cast<T*>(g.d_gate)[group * g.d_gate_ld + c], sum * slope[0].v);
+}
+// The parts that a CTA's warp teams have of groups that they share, in the teams' order: the gradient where the whole group is this CTA's, else this CTA's part.
+// So a group of many short rows leaves a part per CTA and not one per team (200000 rows of 32 values under one gate: 18944 teams, 592 CTAs).
+template <typename T>
+__device__ __forceinline__ void add_parts(const NormGradArgs& g, const float* parts, int apart, int teams_here) {
+    const NormArgs& a = g.f;
+    const int t0 = blockIdx.x * teams_here, from = first_row_of(t0, g.teams, a.rows), to = first_row_of(t0 + teams_here, g.teams, a.rows);
+    float* const mine = g.gate_sums + 2 * static_cast<int64_t>(blockIdx.x) * a.cols;
+    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
+        float sum = 0.f;                          // of the group that the last team has not ended
+        for (int i = 0; i < teams_here; ++i) {
+            const int first = first_row_of(t0 + i, g.teams, a.rows), last = first_row_of(t0 + i + 1, g.teams, a.rows);
+            if (first == last) break;             // teams without rows are all at the end
+            const Group begun(first, a);
+            if (begun.start < first) {
+                sum += parts[2 * i * apart + c];
+                if (begun.end <= last) {
+                    if (begun.start >= from) finish_gate<T>(g, begun.at, c, sum);
+                    else mine[c] = sum;
+                }
+            }
+            const Group open(last - 1, a);
+            if (open.start >= first && open.end > last) sum = parts[(2 * i + 1) * apart + c];
+        }
+        if (from == to) continue;
+        const Group open(to - 1, a);
+        if (open.end > to) mine[(open.start < from ? 0 : a.cols) + c] = sum;
+    }
+}
 
 // GROUPS: a gate for each group of rows, whose gradient is a sum over them.  BIAS: either norm has one, so that the plain sums are needed.
 // SHARED: the parameters are in shared memory (there is no room for them beside one row of five fp32 operands of 8192 values).
@@ -717,7 +767,9 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
                 if (mine && (row + 1 == rows.last || (row + 1) / a.gate_rows != group)) {
                     const int64_t start = static_cast<int64_t>(group) * a.gate_rows, end = min(start + a.gate_rows, static_cast<int64_t>(a.rows));
                     const bool whole = start >= rows.first && end <= rows.last;
-                    float* const part = g.gate_sums + (2 * static_cast<int64_t>(t) + (start < rows.first ? 0 : 1)) * a.cols;
+                    const int which = start < rows.first ? 0 : 1;
+                    float* const part = SIZE ? reinterpret_cast<float*>(dynamic + g.part_bytes) + (2 * team_here + which) * param_cols
+                                             : g.gate_sums + (2 * static_cast<int64_t>(blockIdx.x) + which) * a.cols;
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
                         if (col.has(k)) {
@@ -745,6 +797,8 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
     float* const out = g.sums + static_cast<int64_t>(blockIdx.x) * (BIAS ? 4 : 2) * a.cols;
     float* const column_sums = reinterpret_cast<float*>(dynamic);
     if constexpr (SIZE != 0) __syncthreads();     // nobody reads operands any more
+    if constexpr (SIZE != 0 && GROUPS)
+        if (g.d_gate) add_parts<T>(g, reinterpret_cast<const float*>(dynamic + g.part_bytes), param_cols, kTeamsHere<SIZE>);
     const auto put = [&](float* to, const N (&v)[K][M]) {
         if constexpr (SIZE == 0) {
 #pragma unroll
@@ -773,36 +827,52 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
 struct NormFinishArgs {
     NormGradArgs g;
     int ctas, each;                               // CTAs whose sums there are, and how many sums each has
+    int teams_here;                               // teams of a CTA
     int column_blocks;                            // the grid's first blocks: the parameters; the others: the groups' gates
+    int groups;                                   // of rows under one gate
+    int slices;                                   // of the CTAs that a group spans: a power of two up to kGateSlices
     float *d_scale, *d_post_w, *d_post_b, *d_pre_w, *d_pre_b;      // each may be null
 };
 constexpr int kFinishColumns = 8, kFinishSlices = 64;          // eight columns are a sector
+constexpr int kFinishThreads = kFinishColumns * kFinishSlices;
+constexpr int kGateSlices = 16;                   // 32 columns per block then, four sectors
 
 // The parameters' gradients from the CTAs' sums (8 columns per block, the CTAs in 64 interleaved parts), and the gradients of gates whose rows
-// several teams had.
+// several CTAs had.  Either is a tree of fixed shape over chains that are 1/64 and 1/16 of the CTAs long: one chain over all parts took 1.2 ms and lost
+// twelve bits of a sum of 200000 rows of 32 values (18944 parts then).
 template <typename T>
-__global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_finish(NormFinishArgs q) {
+__global__ void __launch_bounds__(kFinishThreads) k_norm_grad_finish(NormFinishArgs q) {
     __shared__ float part[4][kFinishSlices / 4][kFinishColumns];
+    __shared__ float gate_part[kFinishThreads];
     const NormArgs& a = q.g.f;
     dependency_wait();
     if (static_cast<int>(blockIdx.x) >= q.column_blocks) {
-        // team t begins a group that it does not end: the parts of that group, in the teams' order, for 512 columns per block
-        const int chunks = ceil_div(a.cols, kFinishColumns * kFinishSlices), at = static_cast<int>(blockIdx.x) - q.column_blocks;
-        const int t = at / chunks, c = at % chunks * kFinishColumns * kFinishSlices + threadIdx.x;
-        const int each = a.rows / q.g.teams, more = a.rows % q.g.teams;
-        const auto first_of = [&](int v) { return each * v + min(v, more); };
-        const int first = first_of(t), last = first_of(t + 1);
-        if (first == last || c >= a.cols) return;
-        const int64_t group = (last - 1) / a.gate_rows, start = group * a.gate_rows, end = min(start + a.gate_rows, static_cast<int64_t>(a.rows));
-        if (start < first || end <= last) return;
-        int stop = t + 1;                         // the first team that begins behind the group; teams without rows are all at the end
-        while (stop < q.g.teams && first_of(stop) < end) ++stop;
-        float s = q.g.gate_sums[(2 * static_cast<int64_t>(t) + 1) * a.cols + c];
+        // a group, or where there are more groups than CTAs the one that a CTA has not ended, and some columns
+        const int wide = kFinishThreads / q.slices, chunks = ceil_div(a.cols, wide), at = static_cast<int>(blockIdx.x) - q.column_blocks;
+        const int unit = at / chunks, c = at % chunks * wide + threadIdx.x % wide, slice = threadIdx.x / wide;
+        const auto cta_of = [&](int row) { return team_of(row, q.g.teams, a.rows) / q.teams_here; };
+        int row = unit;
+        if (q.groups <= q.ctas) {
+            row = unit * a.gate_rows;
+        } else {
+            row = first_row_of((unit + 1) * q.teams_here, q.g.teams, a.rows) - 1;
+            if (cta_of(row) != unit) return;      // a CTA without rows
+        }
+        const Group group(row, a);
+        const int first = cta_of(static_cast<int>(group.start)), last = cta_of(static_cast<int>(group.end - 1));
+        if (first == last || (q.groups > q.ctas && first != unit)) return;
+        float s = 0.f;
+        if (c < a.cols) {
+            const float* const sums = q.g.gate_sums + c;
+            if (slice == 0) s = sums[(2 * static_cast<int64_t>(first) + 1) * a.cols];
 #pragma unroll 8                                   // loads that wait for nothing
-        for (int v = t + 1; v < stop; ++v) s += q.g.gate_sums[2 * static_cast<int64_t>(v) * a.cols + c];
-        F1 u[1] = {F1{to_float(static_cast<const T*>(a.gate)[group * a.gate_ld + c])}}, slope[1];
-        with_gate(a.gate_kind, [&](auto kind) { gate_values<T, decltype(kind)::value, true>(u, slope); });
-        from_float(static_cast<T*>(q.g.d_gate)[group * q.g.d_gate_ld + c], s * slope[0].v);
+            for (int v = first + 1 + slice; v <= last; v += q.slices) s += sums[2 * static_cast<int64_t>(v) * a.cols];
+        }
+        gate_part[threadIdx.x] = s;
+        __syncthreads();
+        if (slice != 0 || c >= a.cols) return;
+        for (int i = 1; i < q.slices; ++i) s += gate_part[i * wide + threadIdx.x];
+        finish_gate<T>(q.g, group.at, c, s);
         return;
     }
     const int x = threadIdx.x % kFinishColumns, slice = threadIdx.x / kFinishColumns, c = blockIdx.x * kFinishColumns + x;
@@ -843,7 +913,7 @@ __global__ void __launch_bounds__(kFinishColumns * kFinishSlices) k_norm_grad_fi
 // fit 128 registers, with groups or biases up to five, 168 (100000 rows of 512 fp16 values with groups: 178 us so, 217 with eight values and 128).  Rows of fp32
 // values have eight, as shared memory holds few of them and 16 would leave a CTA half of its warps.
 struct GradPlan {
-    int lanes, values, threads, per_sm, ctas, teams;
+    int lanes, values, threads, per_sm, per_cta, ctas, teams;         // per_cta: teams of a CTA
 };
 constexpr int kMostSms = 160, kMostTeamRows = 1024;          // a team adds at most this many rows in a row
 inline GradPlan grad_plan(int rows, int cols, int type_size, bool many_sums, int sms) {
@@ -854,11 +924,11 @@ inline GradPlan grad_plan(int rows, int cols, int type_size, bool many_sums, int
     // by the registers; shared memory may allow fewer
     p.per_sm = p.lanes ? (p.values > 8 && many_sums ? kGradWarpCtas<16, true> : kGradWarpCtas<8, false>)
                : p.values > 8 && many_sums && p.threads <= kGradThreadsMany ? kGradThreadsMany / p.threads : kGradThreads / p.threads;
-    const int per_cta = p.lanes ? p.threads / p.lanes : 1;
-    const int few = ceil_div(rows, per_cta), many = ceil_div(few, kMostTeamRows), resident = (sms < kMostSms ? sms : kMostSms) * p.per_sm;
+    p.per_cta = p.lanes ? p.threads / p.lanes : 1;
+    const int few = ceil_div(rows, p.per_cta), many = ceil_div(few, kMostTeamRows), resident = (sms < kMostSms ? sms : kMostSms) * p.per_sm;
     p.ctas = resident < many ? many : resident;
     p.ctas = p.ctas < few ? p.ctas : few;
-    p.teams = p.ctas * per_cta;
+    p.teams = p.ctas * p.per_cta;
     return p;
 }
 
@@ -866,7 +936,7 @@ inline GradPlan grad_plan(int rows, int cols, int type_size, bool many_sums, int
 template <typename T>
 bool run_norm(const NormArgs& a, bool packs, int sms, cudaStream_t s);
 template <typename T>
-bool run_norm_grad(NormFinishArgs& q, const GradPlan& plan, bool packs, bool bias, bool groups, int finish_blocks, cudaStream_t s);
+bool run_norm_grad(NormFinishArgs& q, const GradPlan& plan, bool packs, bool bias, bool groups, int64_t finish_blocks, cudaStream_t s);
 
 }  // namespace layers
 }  // namespace cutoff

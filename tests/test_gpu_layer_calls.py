@@ -1,5 +1,5 @@
 """The layer operators in calls that their users may make and that values alone do not cover: warps of which some lanes have no work, launches that the
-runtime refuses, several host threads, tensors that autograd knows; gates far from zero."""
+runtime refuses, several host threads, tensors that autograd knows; gates far from zero, and of very many rows."""
 import ctypes as C
 import threading
 
@@ -268,3 +268,37 @@ def test_autograd_learns_of_results_written_over_what_it_keeps():
         out = torch.empty_like(x)
         binding.dropout(x, 0.5, 1, out=out)
     assert torch.equal(out, binding.dropout(x, 0.5, 1))
+
+
+# ---- gates that many rows share ----------------------------------------------------------------------------------------------------
+# One gate for all rows, and terms of one sign whose sum takes more digits than fp32 has: an addition that follows on too many others rounds the same way
+# over and over.  A sum of n terms in chains and trees of at most `depth` additions is off by depth u of the magnitudes, u = 2^-24.  Rows per team, then at
+# most 32 teams of a CTA, then 16 parts of at most 592 CTAs, then the 16: 11 + 32 + 37 + 16 = 96 for the first case, 22 + 8 + 37 + 16 and 34 + 4 + 28 + 16.
+@pytest.mark.parametrize("rows,cols", [(200000, 24), (100000, 128), (60000, 500)])
+@pytest.mark.parametrize("value", [1 + 2.0 ** -10, 1 + 2.0 ** -9 + 2.0 ** -11])
+def test_a_gate_of_very_many_rows(rows, cols, value):
+    x, h, d = torch.zeros(rows, cols, device="cuda"), torch.ones(rows, cols, device="cuda"), torch.full((rows, cols), value, device="cuda")
+    gate = torch.ones(1, cols, device="cuda")
+    got = binding.residual_norm_grad(x, h, d, None, gate=gate, gate_rows=rows, post=None, pre=None)["gate"]
+    want = rows * value
+    assert np.abs(host(got) - want).max() <= (96 + 1) * U * want
+
+
+# groups on both sides of a team's and of a CTA's rows: a group inside a team, across teams of one CTA, across two CTAs and many
+@pytest.mark.parametrize("rows,cols", [(40000, 24), (9473, 32), (20011, 100), (7000, 512), (1201, 600)])
+@pytest.mark.parametrize("gate_rows", [2, 3, 33, 64, 65, 337, 1000, 9472])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_sums_over_groups(rows, cols, gate_rows, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(rows + gate_rows)
+    dt, groups = TYPES[dtype], -(-rows // gate_rows)
+    x, h = torch.zeros(rows, cols, device="cuda", dtype=dt), torch.ones(rows, cols, device="cuda", dtype=dt)
+    # small whole numbers: every sum is exact in fp32, in any order
+    d = torch.randint(-4, 5, (rows, cols), device="cuda", generator=gen).to(dt)
+    gate = torch.randint(1, 4, (groups, cols), device="cuda", generator=gen).to(dt)
+    kw = dict(gate=gate, gate_rows=gate_rows, post=None, pre=None)
+    got = binding.residual_norm_grad(x, h, d, None, **kw)
+    group = torch.arange(rows, device="cuda") // gate_rows
+    want = torch.zeros(groups, cols, device="cuda").index_add_(0, group, d.float())
+    assert torch.equal(got["gate"], want.to(dt)) and torch.equal(got["x"], d) and torch.equal(got["h"], (d.float() * gate.float()[group]).to(dt))
+    again = binding.residual_norm_grad(x, h, d, None, **kw)
+    assert all(torch.equal(got[k], again[k]) for k in got)
