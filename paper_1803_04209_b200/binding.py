@@ -646,13 +646,13 @@ def dropout(x, p: float, seed: int, step: int = 0, noise_stream: int = STREAM_DR
     residual is the gradient of the result.  p counts in steps of 2^-16.  out may be x or residual."""
     lib = load_library()
     _load_torch()
+    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= noise_stream < 1 << 32 and -1 << 63 <= first_row < 1 << 63):
+        raise ValueError("seed has 64 bits, step and noise_stream 32, first_row 63 and a sign")
     xp, x_ld, rows, cols, device, dtype = _matrix(x, "x")
     code = _type_of(dtype)
     rp, r_ld = _same(residual, "residual", rows, cols, device, dtype)
     given = out
     out, op, o_ld = _result(x, out, "out", rows, cols, device, dtype)
-    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= noise_stream < 1 << 32):
-        raise ValueError("seed has 64 bits, step and noise_stream 32")
     rc = lib.cutoff_dropout(device, code, rows, cols, xp, x_ld, rp, r_ld, op, o_ld, p, seed, step, noise_stream, first_row, _current_stream(device))
     if rc < 0:
         raise CutoffError(rc, "cutoff_dropout")
@@ -664,8 +664,8 @@ def _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post
     """(the layer as bytes, rows, columns, device, type)"""
     if post not in NORMS or pre not in NORMS or gate_kind not in GATES:
         raise ValueError(f"norms: {list(NORMS)}, gates: {list(GATES)}")
-    if gate_rows < 1:
-        raise ValueError("gate_rows is at least 1")
+    if not 1 <= gate_rows < 1 << 63:
+        raise ValueError("gate_rows is at least 1 and less than 2^63")
     xp, x_ld, rows, cols, device, dtype = _matrix(x, "x")
     hp, h_ld = _same(h, "h", rows, cols, device, dtype)
     gp, g_ld = _same(gate, "gate", -(-rows // gate_rows), cols, device, dtype)
@@ -686,6 +686,10 @@ def residual_norm(x, h=None, gate=None, gate_rows: int = 1, gate_kind: str = "li
     residual_out and norm_out may be x or h."""
     lib = load_library()
     _load_torch()
+    if residual_out is not None and h is None:
+        raise ValueError("residual_out: without h there is no block, and r is x")
+    if norm_out is not None and (quantize or not want_norm):
+        raise ValueError("norm_out: no n of x's type is wanted")
     layer, rows, cols, device, dtype = _norm_layer(x, h, gate, gate_rows, gate_kind, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps)
     r, rp, r_ld, n, np_, n_ld, sp = x, None, 0, None, None, 0, None
     if h is not None:

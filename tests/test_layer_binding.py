@@ -33,3 +33,19 @@ def test_tensors_that_require_a_gradient(call):
     with torch.no_grad(), pytest.raises(ValueError) as e:            # then it is their being on the CPU that is refused
         call(_with_gradient)
     assert "requires a gradient" not in str(e.value)
+
+
+# results that the call would not write, and numbers that would arrive as others
+@pytest.mark.parametrize("call,what", [
+    (lambda x: binding.residual_norm(x, residual_out=x), "residual_out"),
+    (lambda x: binding.residual_norm(x, x, want_norm=False, norm_out=x), "norm_out"),
+    (lambda x: binding.residual_norm(x, x, quantize=True, norm_out=x), "norm_out"),
+    (lambda x: binding.residual_norm(x, x, gate=x, gate_rows=1 << 63), "gate_rows"),
+    (lambda x: binding.residual_norm_grad(x, x, x, x, gate=x, gate_rows=1 << 64), "gate_rows"),
+    (lambda x: binding.dropout(x, 0.5, 1, first_row=1 << 64), "first_row"),
+    (lambda x: binding.dropout(x, 0.5, 1, first_row=(1 << 63) + 5), "first_row"),
+    (lambda x: binding.dropout(x, 0.5, 1, first_row=-(1 << 64)), "first_row"),
+])
+def test_what_a_call_would_ignore(call, what):
+    with pytest.raises(ValueError, match=what):
+        call(torch.ones(4, 8))
