@@ -447,8 +447,8 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
  * meaning, and so NaN or infinity in its products.
  *
  * cutoff_quantized_product: y[i][j] = (sum_k a[i][k] b[j][k]) * a_scale[i] * b_scale[j] + bias[j], y m x n of `type`; the sum is exact.  a: m x k,
- * b: n x k int8; both start on 16 bytes and their leading dimensions are multiples of 16 (BAD_ARG otherwise); what lies behind a row's k values
- * is not used.  bias: n floats or NULL.
+ * b: n x k int8; both start on 16 bytes and, with more than one row, their leading dimensions are multiples of 16 (BAD_ARG otherwise); what lies
+ * behind a row's k values is not used.  bias: n floats or NULL.
  * m <= 2^30; k <= CUTOFF_PRODUCT_MAX_K (TOO_LARGE otherwise: the sum could leave 32 bits); n, and cols of cutoff_quantize_rows, <= 2^30 (TOO_LARGE).
  * The tensor-core kernels' waits are bounded: a tile whose operands do not arrive within seconds (a hung device) is written as NaN, as are a norm's rows.
  * Errors of both: BAD_ARG, TOO_LARGE, CUDA. */

@@ -340,6 +340,9 @@ int cutoff_quantize_rows(int device, int32_t type, int64_t rows, int32_t cols, c
 
 int cutoff_quantized_product(int device, int64_t m, int32_t n, int32_t k, const int8_t* a, int64_t a_ld, const float* a_scale, const int8_t* b,
                              int64_t b_ld, const float* b_scale, const float* bias, int32_t type, void* y, int64_t y_ld, void* stream) {
+    // a single row has no distance to a next one; tensor maps want one all the same
+    if (m == 1 && a_ld >= k && a_ld <= kMostApart) a_ld = (a_ld + 15) / 16 * 16;
+    if (n == 1 && b_ld >= k && b_ld <= kMostApart) b_ld = (b_ld + 15) / 16 * 16;
     if (device < 0 || m < 0 || m > kMostRows || n < 1 || k < 1 || !a || !a_scale || !b || !b_scale || !known_type(type) || !y || bad_matrix(a, a_ld, k, 1) ||
         bad_matrix(b, b_ld, k, 1) || bad_matrix(y, y_ld, n, type_size(type)) || off(a_scale, 4) || off(b_scale, 4) || off(bias, 4) || !rows_aligned(a, a_ld, 1, 16) || !rows_aligned(b, b_ld, 1, 16))
         return CUTOFF_ERR_BAD_ARG;

@@ -302,3 +302,20 @@ def test_sums_over_groups(rows, cols, gate_rows, dtype):
     assert torch.equal(got["gate"], want.to(dt)) and torch.equal(got["x"], d) and torch.equal(got["h"], (d.float() * gate.float()[group]).to(dt))
     again = binding.residual_norm_grad(x, h, d, None, **kw)
     assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+# ---- single rows -------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("k", [1, 17, 513, 1001, 4095])
+def test_the_distance_of_a_single_row_may_be_any(k):
+    gen = torch.Generator(device="cuda").manual_seed(k)
+    token = torch.randint(-127, 128, (1, k), dtype=torch.int8, device="cuda", generator=gen)               # contiguous, as its owner has it
+    many = torch.randint(-127, 128, (40, (k + 15) // 16 * 16), dtype=torch.int8, device="cuda", generator=gen)[:, :k]
+    one, scales = torch.ones(1, device="cuda"), torch.ones(40, device="cuda")
+    want = (token.long().cpu() @ many.long().cpu().T).float()                                               # below 2^27: rounded once
+    assert torch.equal(binding.quantized_product((token, one), (many, scales), dtype=torch.float32).cpu(), want)
+    assert torch.equal(binding.quantized_product((many, scales), (token, one), dtype=torch.float32).cpu(), want.T)
+    square = (token.long() ** 2).sum().float()
+    assert torch.equal(binding.quantized_product((token, one), (token, one), dtype=torch.float32)[0, 0], square)
+    with pytest.raises(binding.CutoffError) as e:                                                           # two rows are a distance apart
+        binding.quantized_product((torch.zeros(2, 17, dtype=torch.int8, device="cuda"), scales[:2]), (torch.zeros(1, 17, dtype=torch.int8, device="cuda"), one))
+    assert e.value.code == binding.ERR_BAD_ARG
