@@ -2,6 +2,7 @@
 // work is enqueued.
 #include "../../include/cutoff.h"
 
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -27,14 +28,13 @@ int done(bool ok) {
 }
 
 int sm_count(int device) {
-    static int sms[kMostDevices] = {};
+    static std::atomic<int> sms[kMostDevices] = {};       // the same for every host thread
     if (device >= kMostDevices) return 148;
-    if (!sms[device]) {
-        int v = 0;
-        if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || v < 1) return 148;
-        sms[device] = v;
-    }
-    return sms[device];
+    int v = sms[device].load(std::memory_order_relaxed);
+    if (v > 0) return v;
+    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || v < 1) return 148;
+    sms[device].store(v, std::memory_order_relaxed);
+    return v;
 }
 
 bool known_type(int32_t type) { return type == CUTOFF_TYPE_FP32 || type == CUTOFF_TYPE_FP16 || type == CUTOFF_TYPE_BF16; }

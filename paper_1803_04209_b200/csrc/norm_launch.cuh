@@ -76,7 +76,8 @@ bool launch_norm(const NormArgs& a, int sms, cudaStream_t s) {
         if (ctas <= sms * st.per_sm) st.stages = 1, st.bytes = stage + gate;  // a row each
         ops.stages = st.stages;
         if (!allow_smem(kernel, st.bytes)) return;
-        ok = launch_plain(kernel, dim3(ctas < sms * st.per_sm ? ctas : sms * st.per_sm), dim3(threads), st.bytes, s, a, ops, st.stages * stage) == cudaSuccess;
+        const int grid = ctas < sms * st.per_sm ? ctas : sms * st.per_sm;
+        ok = launch_plain(kernel, dim3(grid), dim3(threads), st.bytes, s, a, ops, st.stages * stage, grid <= sms) == cudaSuccess;
     });
     return ok;
 }

@@ -28,7 +28,6 @@ enum : int { kNormNone = 0, kNormRms = 1, kNormLayer = 2 };
 enum : int { kGateLinear = 0, kGateSigmoid = 1, kGateSilu = 2 };
 
 constexpr int kMostRows = 1 << 30;
-constexpr int kFewCtas = 148;
 
 struct NormArgs {
     const void *x, *h, *gate;                     // h: null = no block before (r = x); gate: null = 1
@@ -319,12 +318,12 @@ constexpr int kNormRegisters = V * K > 8 ? (MORE ? 96 : 80) : (MORE ? 80 : 64);
 
 // The parameters of a thread's columns stay in its registers.
 template <typename T, int V, int K, int SIZE, bool LAYER, bool BIAS, bool GROUPS>
-__global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands, int gate_bytes) {
+__global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormArgs a, const __grid_constant__ RowOperands operands, int gate_bytes, bool few) {
     using N = Num<V>;
     constexpr int M = kNums<V>, kBias = BIAS ? K : 1;
     CUTOFF_NORM_TEAM(a, operands)
-    // With at most a CTA per SM the successor, a product of few tokens perhaps, may set itself up meanwhile; the CTAs of a large one would crowd on some SMs.
-    if (gridDim.x <= kFewCtas) launch_dependents();
+    // With at most a CTA per SM (few) the successor, a product of few tokens perhaps, may set itself up meanwhile; the CTAs of a large one would crowd on some SMs.
+    if (few) launch_dependents();
     const int at_h = 1, at_gate = 2;
     const int t = blockIdx.x * kTeamsHere<SIZE> + team_here, teams = gridDim.x * kTeamsHere<SIZE>;
     const TeamRows<GROUPS> rows(t, teams, a.rows);
@@ -530,7 +529,6 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
     // places of the operands in a stage
     const bool has_gate_rows = !GROUPS && a.gate != nullptr;
     const int at_h = 1, at_gate = at_h + (a.h != nullptr), at_r = at_gate + has_gate_rows, at_n = at_r + (g.d_r != nullptr);
-    dependency_wait();
     bool failed = false;                          // a wait gave up: none is made after it, and nothing is asked for
     for (int s = 0; s < operands.stages; ++s)
         if (rows.has(s)) pipe.fetch(s, rows(s), team);
