@@ -300,7 +300,7 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
         q.groups = ceil_div64(g.f.rows, g.f.gate_rows);
         q.slices = 1;
         while (q.slices < kGateSlices && 8 * q.slices < spans && 8 * q.slices < plan.ctas) q.slices *= 2;
-        gate_blocks = static_cast<int64_t>(q.groups < plan.ctas ? q.groups : plan.ctas) * ceil_div(g.f.cols, kFinishThreads / q.slices);
+        gate_blocks = static_cast<int64_t>(q.groups < plan.ctas ? q.groups : plan.ctas) * ceil_div(g.f.cols, kGateColumns * (kFinishThreads / q.slices));
     }
     bool ok = false;
     with_type(layer->type, [&](auto t) { ok = run_norm_grad<decltype(t)>(q, plan, packs, bias, groups, q.column_blocks + gate_blocks, s); });

@@ -41,33 +41,40 @@ struct NormArgs {
     int64_t r_ld, n_ld;
 };
 
-// 1 / (1 + exp(-g)) and, with SLOPE, its derivative, both from u = exp(-|g|) <= 1 and s = 1 / (1 + u): the value is s or u s, and the derivative u s s and
-// not a difference value - value^2, of which nothing is left where the value is close to 1.  fp32: u to two units of the last place, value within six and
-// derivative within eight of them, whatever the gate.  What is rounded to 16 bits takes the hardware's exponential of |g| log2(e), a few instructions
-// less for each value: within 2 |g| + 10 units of 2^-24, a hundredth of its own rounding, and zero below 2^-126.
-template <typename T, bool SLOPE>
+// 1 / (1 + exp(-g)) and, with SLOPE, its derivative as a product, not as value - value^2, of which nothing is left where the value is close to 1.
+// EXACT, for fp32: from u = exp(-|g|), which is two units of the last place off, and s = 1 / (1 + u): s or u s, within six units, and u s s, within
+// eight, whatever the gate.  Otherwise, for what is rounded to 16 bits: the hardware's exponential of -g log2(e), e, at a third of the instructions:
+// s = 1 / (1 + e) within 2 |g| + 10 units of 2^-24, a hundredth of its own rounding, and e s s; zero below 2^-126 (e stops at 2^127: infinity times
+// zero would be NaN).  100000 x 512 fp32 values with gates, gradients: 326 us if nothing is EXACT, 351 with the derivatives so; 16-bit types gain 7 %.
+template <bool EXACT, bool SLOPE>
 __device__ __forceinline__ float logistic(float g, float& slope) {
-    float u, s;
-    if constexpr (sizeof(T) == 4) u = expf(-fabsf(g));
-    else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(u) : "f"(fabsf(g) * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + u));
-    const float small = u * s;
-    if constexpr (SLOPE) slope = small * s;
-    return g < 0.f ? small : s;
+    float e, s;
+    if constexpr (EXACT) {
+        e = expf(-fabsf(g));
+    } else {
+        float t = g * -1.4426950408889634f;
+        if constexpr (SLOPE) asm("min.NaN.f32 %0, %0, %1;" : "+f"(t) : "f"(127.f));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+    }
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
+    if constexpr (SLOPE) slope = e * s * s;
+    return EXACT ? (g < 0.f ? e : 1.f) * s : s;
 }
-template <typename T, bool SLOPE>
-__device__ __forceinline__ F1 logistic(F1 g, F1& slope) { return F1{logistic<T, SLOPE>(g.v, slope.v)}; }
-template <typename T, bool SLOPE>
+template <bool EXACT, bool SLOPE>
+__device__ __forceinline__ F1 logistic(F1 g, F1& slope) { return F1{logistic<EXACT, SLOPE>(g.v, slope.v)}; }
+template <bool EXACT, bool SLOPE>
 __device__ __forceinline__ F2 logistic(F2 g, F2& slope) {
     float x, y, s = 0.f, t = 0.f;
     unpack2(g.v, x, y);
-    x = logistic<T, SLOPE>(x, s);
-    y = logistic<T, SLOPE>(y, t);
+    x = logistic<EXACT, SLOPE>(x, s);
+    y = logistic<EXACT, SLOPE>(y, t);
     if constexpr (SLOPE) slope.v = pack2(s, t);
     return F2{pack2(x, y)};
 }
-// g, a gate of type T, becomes act(g), and with SLOPE slope its derivative.
-template <typename T, int KIND, bool SLOPE, typename N, int M>
+template <typename T>
+constexpr bool kExactGate = sizeof(T) == 4;
+// g becomes act(g), and with SLOPE slope its derivative.
+template <bool EXACT, int KIND, bool SLOPE, typename N, int M>
 __device__ __forceinline__ void gate_values(N (&g)[M], N (&slope)[M]) {
 #pragma unroll
     for (int i = 0; i < M; ++i) {
@@ -75,7 +82,7 @@ __device__ __forceinline__ void gate_values(N (&g)[M], N (&slope)[M]) {
             if constexpr (SLOPE) slope[i] = splat<N>(1.f);
         } else {
             N d;
-            const N s = logistic<T, SLOPE>(g[i], d);
+            const N s = logistic<EXACT, SLOPE>(g[i], d);
             if constexpr (KIND == kGateSigmoid) {
                 g[i] = s;
                 if constexpr (SLOPE) slope[i] = d;
@@ -285,7 +292,7 @@ struct GroupGate {
         with_gate(a.gate_kind, [&](auto kind) {
             put([&](int k, Num<V> (&u)[kNums<V>]) {
                 read_global<T, V>(row + (col.has(k) ? col(k) : 0), u);
-                gate_values<T, decltype(kind)::value, false>(u, u);
+                gate_values<kExactGate<T>, decltype(kind)::value, false>(u, u);
                 if (!col.has(k))
 #pragma unroll
                     for (int i = 0; i < kNums<V>; ++i) u[i] = splat<Num<V>>(0.f);
@@ -391,7 +398,7 @@ __global__ void __maxnreg__((kNormRegisters<V, K, BIAS>)) k_residual_norm(NormAr
                     for (int k = 0; k < K; ++k) {
                         N t[M];
                         take<T, V>(gate_at, col, k, columns, t);
-                        gate_values<T, decltype(kind)::value, false>(t, t);
+                        gate_values<kExactGate<T>, decltype(kind)::value, false>(t, t);
                         add_x(k, t);
                     }
                 });
@@ -478,7 +485,7 @@ template <typename T>
 __device__ __forceinline__ void finish_gate(const NormGradArgs& g, int group, int c, float sum) {
     const NormArgs& a = g.f;
     F1 u[1] = {F1{to_float(static_cast<const T*>(a.gate)[group * a.gate_ld + c])}}, slope[1];
-    with_gate(a.gate_kind, [&](auto kind) { gate_values<T, decltype(kind)::value, true>(u, slope); });
+    with_gate(a.gate_kind, [&](auto kind) { gate_values<kExactGate<T>, decltype(kind)::value, true>(u, slope); });
     from_float(static_cast<T*>(g.d_gate)[group * g.d_gate_ld + c], sum * slope[0].v);
 }
 // The parts that a CTA's warp teams have of groups that they share, in the teams' order: the gradient where the whole group is this CTA's, else this CTA's part.
@@ -631,7 +638,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
                         for (int k = 0; k < K; ++k) {
                             N t[M];
                             take<T, V>(gate_at, col, k, columns, t);
-                            gate_values<T, decltype(kind)::value, false>(t, t);
+                            gate_values<false, decltype(kind)::value, false>(t, t);      // a summand of r: what counts is its absolute error, 2 u at most
                             add_x(k, t);
                         }
                     });
@@ -729,7 +736,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
                         N w[M], u[M], slope[M], p[M];
                         param_of(0, k, w);
                         take<T, V>(gate_at, col, k, columns, u);
-                        gate_values<T, decltype(kind)::value, true>(u, slope);
+                        gate_values<kExactGate<T>, decltype(kind)::value, true>(u, slope);
                         branch_of(k, w, p);
 #pragma unroll
                         for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], mul(d[k][i], p[i]));
@@ -774,7 +781,7 @@ __global__ void __launch_bounds__(SIZE ? kNormWarpThreads : THREADS, SIZE ? kGra
                             if (whole) {
                                 N u[M], slope[M];
                                 read_global<T, V>(static_cast<const T*>(a.gate) + group * a.gate_ld + col(k), u);
-                                with_gate(a.gate_kind, [&](auto kind) { gate_values<T, decltype(kind)::value, true>(u, slope); });
+                                with_gate(a.gate_kind, [&](auto kind) { gate_values<kExactGate<T>, decltype(kind)::value, true>(u, slope); });
 #pragma unroll
                                 for (int i = 0; i < M; ++i) slope[i] = mul(slope[i], gate_sum[k][i]);
                                 if (g.d_gate) write_global<T, V>(static_cast<T*>(g.d_gate) + group * g.d_gate_ld, col(k), a.cols, slope);
@@ -833,7 +840,8 @@ struct NormFinishArgs {
 };
 constexpr int kFinishColumns = 8, kFinishSlices = 64;          // eight columns are a sector
 constexpr int kFinishThreads = kFinishColumns * kFinishSlices;
-constexpr int kGateSlices = 16;                   // 32 columns per block then, four sectors
+constexpr int kGateSlices = 16;                   // 32 columns at a time then, four sectors
+constexpr int kGateColumns = 4;                   // of a thread: a block finds out its CTAs by some ten divisions, which a block for each 512 columns paid too often (638 x 5248, 11 us)
 
 // The parameters' gradients from the CTAs' sums (8 columns per block, the CTAs in 64 interleaved parts), and the gradients of gates whose rows
 // several CTAs had.  Either is a tree of fixed shape over chains that are 1/64 and 1/16 of the CTAs long: one chain over all parts took 1.2 ms and lost
@@ -841,36 +849,49 @@ constexpr int kGateSlices = 16;                   // 32 columns per block then, 
 template <typename T>
 __global__ void __launch_bounds__(kFinishThreads) k_norm_grad_finish(NormFinishArgs q) {
     __shared__ float part[4][kFinishSlices / 4][kFinishColumns];
-    __shared__ float gate_part[kFinishThreads];
+    __shared__ float gate_part[kGateColumns][kFinishThreads];
     const NormArgs& a = q.g.f;
     dependency_wait();
     if (static_cast<int>(blockIdx.x) >= q.column_blocks) {
         // a group, or where there are more groups than CTAs the one that a CTA has not ended, and some columns
-        const int wide = kFinishThreads / q.slices, chunks = ceil_div(a.cols, wide), at = static_cast<int>(blockIdx.x) - q.column_blocks;
-        const int unit = at / chunks, c = at % chunks * wide + threadIdx.x % wide, slice = threadIdx.x / wide;
-        const auto cta_of = [&](int row) { return team_of(row, q.g.teams, a.rows) / q.teams_here; };
-        int row = unit;
-        if (q.groups <= q.ctas) {
+        const int wide = kFinishThreads / q.slices, chunks = ceil_div(a.cols, kGateColumns * wide), at = static_cast<int>(blockIdx.x) - q.column_blocks;
+        const int unit = at / chunks, c0 = at % chunks * kGateColumns * wide + threadIdx.x % wide, slice = threadIdx.x / wide;
+        const bool by_group = q.groups <= q.ctas;
+        int row, first = unit;
+        if (by_group) {
             row = unit * a.gate_rows;
         } else {
             row = first_row_of((unit + 1) * q.teams_here, q.g.teams, a.rows) - 1;
-            if (cta_of(row) != unit) return;      // a CTA without rows
+            if (row < first_row_of(unit * q.teams_here, q.g.teams, a.rows)) return;       // a CTA without rows
         }
         const Group group(row, a);
-        const int first = cta_of(static_cast<int>(group.start)), last = cta_of(static_cast<int>(group.end - 1));
-        if (first == last || (q.groups > q.ctas && first != unit)) return;
-        float s = 0.f;
-        if (c < a.cols) {
-            const float* const sums = q.g.gate_sums + c;
-            if (slice == 0) s = sums[(2 * static_cast<int64_t>(first) + 1) * a.cols];
-#pragma unroll 8                                   // loads that wait for nothing
-            for (int v = first + 1 + slice; v <= last; v += q.slices) s += sums[2 * static_cast<int64_t>(v) * a.cols];
+        if (by_group) first = team_of(row, q.g.teams, a.rows) / q.teams_here;
+        const int behind = first_row_of((first + 1) * q.teams_here, q.g.teams, a.rows);   // the CTA's last row, and one
+        if (group.end <= behind || group.start < first_row_of(first * q.teams_here, q.g.teams, a.rows)) return;      // one CTA's, or begun by another
+        const int last = team_of(static_cast<int>(group.end) - 1, q.g.teams, a.rows) / q.teams_here;
+        float s[kGateColumns];
+#pragma unroll
+        for (int i = 0; i < kGateColumns; ++i) {
+            const int c = c0 + i * wide;
+            s[i] = slice == 0 && c < a.cols ? q.g.gate_sums[(2 * static_cast<int64_t>(first) + 1) * a.cols + c] : 0.f;
         }
-        gate_part[threadIdx.x] = s;
-        __syncthreads();
-        if (slice != 0 || c >= a.cols) return;
-        for (int i = 1; i < q.slices; ++i) s += gate_part[i * wide + threadIdx.x];
-        finish_gate<T>(q.g, group.at, c, s);
+#pragma unroll 2                                   // loads that wait for nothing
+        for (int v = first + 1 + slice; v <= last; v += q.slices)
+#pragma unroll
+            for (int i = 0; i < kGateColumns; ++i)
+                if (c0 + i * wide < a.cols) s[i] += q.g.gate_sums[2 * static_cast<int64_t>(v) * a.cols + c0 + i * wide];
+        if (q.slices > 1) {
+#pragma unroll
+            for (int i = 0; i < kGateColumns; ++i) gate_part[i][threadIdx.x] = s[i];
+            __syncthreads();
+            if (slice != 0) return;
+#pragma unroll
+            for (int i = 0; i < kGateColumns; ++i)
+                for (int j = 1; j < q.slices; ++j) s[i] += gate_part[i][j * wide + threadIdx.x];
+        }
+#pragma unroll
+        for (int i = 0; i < kGateColumns; ++i)
+            if (c0 + i * wide < a.cols) finish_gate<T>(q.g, group.at, c0 + i * wide, s[i]);
         return;
     }
     const int x = threadIdx.x % kFinishColumns, slice = threadIdx.x / kFinishColumns, c = blockIdx.x * kFinishColumns + x;
