@@ -374,7 +374,7 @@ enum { CUTOFF_GATE_LINEAR = 0, CUTOFF_GATE_SIGMOID = 1, CUTOFF_GATE_SILU = 2 };
  * residual.  Guide, transition and emission use the streams below 0x400.
  *   x, y      device, rows x cols;  residual  device, rows x cols, or NULL for zeros
  *   p         0 .. 1; with T = 65536 everything is dropped.  A dropped value is not looked at: NaN or infinity there do no harm.
- *   first_row + rows <= 2^32, cols <= 2^30 (TOO_LARGE otherwise).  Errors: BAD_ARG, TOO_LARGE, CUDA. */
+ *   first_row + rows <= 2^32 (BAD_ARG otherwise), cols <= 2^30 (TOO_LARGE otherwise).  Errors: BAD_ARG, TOO_LARGE, CUDA. */
 int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const void* x, int64_t x_ld, const void* residual,
                    int64_t residual_ld, void* y, int64_t y_ld, double p, uint64_t seed, uint32_t step, uint32_t noise_stream, int64_t first_row,
                    void* stream);
@@ -384,8 +384,9 @@ int cutoff_dropout(int device, int32_t type, int64_t rows, int32_t cols, const v
  * where post and pre are CUTOFF_NORM_*: RMS v / sqrt(mean(v^2) + eps), LAYER (v - mean(v)) / sqrt(var(v) + eps) (population variance), times the weight
  * plus the bias (NULL: ones, zeros), or NONE, which still applies weight and bias.  gate is a row for every gate_rows rows of x (1: one for each
  * row; the last group may be shorter); act is CUTOFF_GATE_*: g, 1 / (1 + exp(-g)), g / (1 + exp(-g)).  fp32: act within 6 units of the last place for any
- * gate; 16-bit types: act within (2 |g| + 11) 2^-24 of itself before the result is rounded, zero where the sigmoid is below 2^-126.  NULL: gate 1, scale 1.  With h NULL
- * there is no block: r = x (scale, gate, post_weight and post_bias must be NULL).  rows <= 2^30, cols <= 8192 (TOO_LARGE otherwise), eps > 0.
+ * gate, its derivative within 8; 16-bit types: act within (2 |g| + 11) 2^-24 of itself before the result is rounded, zero where the sigmoid is below 2^-126.  NULL: gate 1, scale 1.  With h NULL
+ * there is no block: r = x (scale, gate, post_weight and post_bias must be NULL).  rows <= 2^30 (BAD_ARG otherwise), cols <= 8192 (TOO_LARGE otherwise), eps > 0
+ * and finite.
  *
  * cutoff_residual_norm: residual (rows x cols, receives r; NULL = not wanted; must be NULL without h) and norm (receives n; NULL = not wanted).
  * With norm_scale (rows floats) n is not stored as `type` but as 8-bit integers as cutoff_quantize_rows makes them of the unrounded n, norm being
@@ -449,7 +450,8 @@ int cutoff_residual_norm_grad(int device, const cutoff_norm_layer* layer, const 
  * cutoff_quantized_product: y[i][j] = (sum_k a[i][k] b[j][k]) * a_scale[i] * b_scale[j] + bias[j], y m x n of `type`; the sum is exact.  a: m x k,
  * b: n x k int8; both start on 16 bytes and, with more than one row, their leading dimensions are multiples of 16 (BAD_ARG otherwise); what lies
  * behind a row's k values is not used.  bias: n floats or NULL.
- * m <= 2^30; k <= CUTOFF_PRODUCT_MAX_K (TOO_LARGE otherwise: the sum could leave 32 bits); n, and cols of cutoff_quantize_rows, <= 2^30 (TOO_LARGE).
+ * m <= 2^30, rows of cutoff_quantize_rows < 2^31 (BAD_ARG otherwise); k <= CUTOFF_PRODUCT_MAX_K (TOO_LARGE otherwise: the sum could leave 32 bits); n, and
+ * cols of cutoff_quantize_rows, <= 2^30 (TOO_LARGE).
  * The tensor-core kernels' waits are bounded: a tile whose operands do not arrive within seconds (a hung device) is written as NaN, as are a norm's rows.
  * Errors of both: BAD_ARG, TOO_LARGE, CUDA. */
 #define CUTOFF_PRODUCT_MAX_K 131071

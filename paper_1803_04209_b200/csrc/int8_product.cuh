@@ -2,7 +2,7 @@
 //
 //   y[i][j] = (sum over k of a[i][k] b[j][k]) * a_scale[i] * b_scale[j] + bias[j]
 //
-// The sums are exact (32-bit integers, at most 131072 products of magnitudes up to 128), so no split or order of them changes a result; they are
+// The sums are exact (32-bit integers, at most 131071 products of magnitudes up to 128: 131072 would be 2^31), so no split or order of them changes a result; they are
 // scaled in fp32 and rounded once when stored.
 //
 // k_quantize_rows brings rows of fp32, fp16 or bf16 values into that form.

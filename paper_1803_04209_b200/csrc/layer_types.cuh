@@ -363,8 +363,8 @@ __host__ __device__ inline int slot_bytes_of(int row_bytes, int team_threads, in
 }
 
 // 8-bit integers of a row whose largest magnitude has these bits (compared as an integer, so that a NaN is the largest of all): value =
-// integer * scale, integer = rint(value * inverse).  A row of magnitudes below 2^-100 counts as zeros, because 127 / top would leave the range;
-// one with an infinity or a NaN has a scale that is not finite either, and integers of no meaning.
+// integer * scale, integer = rint(value * inverse).  A row of magnitudes below 2^-100 counts as zeros: 127 / top leaves the range of fp32 below 2^-121 and
+// top / 127 its normal numbers below 2^-119, and the border keeps some distance from both.  One with an infinity or a NaN has a scale that is not finite either, and integers of no meaning.
 struct RowScale {
     float scale, inverse;
 };

@@ -9,14 +9,14 @@
 //
 // A row belongs to a team, 4 to 32 lanes of a warp (rows of up to 512 values) or a CTA, that goes through many rows; the asynchronous copy engine brings
 // the operands of the next row into shared memory meanwhile (RowPipe).  The backward pass keeps the parameters' sums of a thread's columns in
-// registers; k_norm_grad_finish adds the CTAs' sums in their order, so that results are the same on every run.
+// registers; k_norm_grad_finish adds the CTAs' sums in a tree of fixed shape, so that results are the same on every run.
 //
 // What bounds it (4096 bf16 values, 16384 rows, a gate value for each): the forward pass the memory, 0.67 GB in 108 us, 95 % of a copy's rate; the
-// backward pass, 1.07 GB in 224 us (73 %), its instructions, some 55 per value and as many as 16 warps of 128 registers issue between three sums
-// over the CTA per row.  What made it so, in us: operands in registers 341 and 703; staged by cp.async 157 and 357; by bulk copies, with two values per
+// backward pass, 1.07 GB in 225 us (73 %), its instructions, some 55 per value and as many as 16 warps of 128 registers issue between four sums
+// over the CTA per row (RMS norms; layer norms take two more).  What made it so, in us: operands in registers 341 and 703; staged by cp.async 157 and 357; by bulk copies, with two values per
 // instruction and parameters in registers or shared memory (in the L1, beside the operands, there is no room for them) 153 and 281; predicates beside the accesses and one branch
 // on the gate's kind per row instead of one for each pack 108 and 224.  Odd rows pay for single values: 5000 rows of 2175 fp32 values with
-// layer norms, biases and a gate for every 125 rows 53 us (floor 27), the gradients of 4001 x 1025 63 us (floor 15).  Not kept: consecutive rows per team
+// layer norms, biases and a gate for every 125 rows 53 us (floor 27), the gradients of 4001 x 1025 58 us (floor 15).  Not kept: consecutive rows per team
 // where nothing asks for them (150 us against 106); single values in pairs a team apart, two to an instruction (no gain: latency bounds those rows).
 #pragma once
 #include "layer_types.cuh"
@@ -45,7 +45,8 @@ struct NormArgs {
 // EXACT, for fp32: from u = exp(-|g|), which is two units of the last place off, and s = 1 / (1 + u): s or u s, within six units, and u s s, within
 // eight, whatever the gate.  Otherwise, for what is rounded to 16 bits: the hardware's exponential of -g log2(e), e, at a third of the instructions:
 // s = 1 / (1 + e) within 2 |g| + 10 units of 2^-24, a hundredth of its own rounding, and e s s; zero below 2^-126 (e stops at 2^127: infinity times
-// zero would be NaN).  100000 x 512 fp32 values with gates, gradients: 326 us if nothing is EXACT, 351 with the derivatives so; 16-bit types gain 7 %.
+// zero would be NaN).  100000 x 512 fp32 values with gates, gradients: 325 us if nothing is EXACT, 345 as it is; 60000 x 333 fp16
+// 139 us so and 149 with EXACT's form.
 template <bool EXACT, bool SLOPE>
 __device__ __forceinline__ float logistic(float g, float& slope) {
     float e, s;
@@ -319,7 +320,8 @@ struct TeamRows {
     __device__ __forceinline__ bool has(int turn) const { return (*this)(turn) < last; }
 };
 
-// Registers of a forward thread: with 16 values and their parameters 80, three CTAs of 256 threads per SM.
+// Registers of a forward thread: with 16 values and their parameters 80, three CTAs of 256 threads per SM.  With biases 96, and the form of odd rows with
+// layer norms and groups still spills 144 bytes per thread, warp teams of 16 single values up to 308.
 template <int V, int K, bool MORE>
 constexpr int kNormRegisters = V * K > 8 ? (MORE ? 96 : 80) : (MORE ? 80 : 64);
 
