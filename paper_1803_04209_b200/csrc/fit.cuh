@@ -202,7 +202,9 @@ struct RnnArgs {
     int chunk;                      // k rows of the weights in shared memory at a time (H: all of them, loaded once)
 };
 
+// The barrier takes whole warps (.aligned), whose lanes may come from branches: they meet first.
 __device__ __forceinline__ void cluster_sync() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t cluster_rank() {

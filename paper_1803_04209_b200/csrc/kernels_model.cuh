@@ -389,7 +389,8 @@ k_enc_rnn_cluster(ModelDev m, const float* __restrict__ proj, const DevState* __
         for (int idx = threadIdx.x; idx < W * R; idx += blockDim.x)
             sproj[idx] = window_projection(m, proj, dir, idx / R, static_cast<int>(rank) * R + idx % R, pushes, inv_scale);
     }
-    // every CTA of the cluster has started and initialised its buffers before anyone writes into them
+    // every CTA of the cluster has started and initialised its buffers before anyone writes into them; the barrier takes whole warps, whose lanes meet first
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     const float* wrow = sW + static_cast<size_t>(row) * ldw;
     int cur = 0;
@@ -416,6 +417,7 @@ k_enc_rnn_cluster(ModelDev m, const float* __restrict__ proj, const DevState* __
             asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v) : "memory");
         }
         if (part == 0) hlr[(static_cast<size_t>(dir) * W + t) * H + i] = v;
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         cur ^= 1;
     }

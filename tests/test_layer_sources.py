@@ -1,4 +1,4 @@
-"""What the sources of the layer operators' tensor-core kernels have to say, because no run would show it for certain."""
+"""What the sources of kernels in clusters and on the tensor cores have to say, because no run would show it for certain."""
 import os
 import re
 
@@ -13,7 +13,7 @@ def _source(name: str) -> str:
 
 
 # A barrier of the cluster, or of some of a CTA's warps, takes whole warps (.aligned), and lanes leave a branch when they like.
-@pytest.mark.parametrize("name", ["tcgen05.cuh", "int8_tc.cuh"])
+@pytest.mark.parametrize("name", ["tcgen05.cuh", "int8_tc.cuh", "kernels_model.cuh", "fit.cuh"])
 def test_lanes_meet_before_a_barrier_that_takes_whole_warps(name):
     source = _source(name)
     found = list(re.finditer(r'asm volatile\("(?:barrier\.cluster\.arrive[^"]*\.aligned|bar\.sync)[^"]*"', source))
