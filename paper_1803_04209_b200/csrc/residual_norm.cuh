@@ -847,7 +847,7 @@ constexpr int kGateColumns = 4;                   // of a thread: a block finds 
 
 // The parameters' gradients from the CTAs' sums (8 columns per block, the CTAs in 64 interleaved parts), and the gradients of gates whose rows
 // several CTAs had.  Either is a tree of fixed shape over chains that are 1/64 and 1/16 of the CTAs long: one chain over all parts took 1.2 ms and lost
-// twelve bits of a sum of 200000 rows of 32 values (18944 parts then).
+// eleven bits of a sum of 200000 rows of 32 values (18944 parts then).
 template <typename T>
 __global__ void __launch_bounds__(kFinishThreads) k_norm_grad_finish(NormFinishArgs q) {
     __shared__ float part[4][kFinishSlices / 4][kFinishColumns];
